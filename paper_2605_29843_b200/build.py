@@ -7,10 +7,12 @@ import os
 import subprocess
 import sys
 import sysconfig
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libharp.so")
+OBJECTS = os.path.join(HERE, "_build")
 CALL, CALL_SRC = os.path.join(HERE, "_harpcall.abi3.so"), os.path.join(HERE, "csrc", "pycall.c")
 
 
@@ -18,12 +20,16 @@ def sources():
     return sorted(glob.glob(os.path.join(HERE, "csrc", "*.cu")))
 
 
+def headers_of_sources():
+    return glob.glob(os.path.join(HERE, "csrc", "*.h")) + glob.glob(os.path.join(HERE, "csrc", "*.cuh")) \
+        + glob.glob(os.path.join(ROOT, "include", "*.h"))
+
+
 def _stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = sources() + glob.glob(os.path.join(HERE, "csrc", "*.h")) + glob.glob(os.path.join(HERE, "csrc", "*.cuh")) \
-        + glob.glob(os.path.join(ROOT, "include", "*.h"))
+    deps = sources() + headers_of_sources()
     return any(os.path.getmtime(p) > t for p in deps)
 
 
@@ -34,7 +40,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if not force and not _stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc, "-shared", "-Xcompiler", "-fPIC", "-std=c++17", "-O3", "-lineinfo",
+    cmd = [nvcc, "-c", "-Xcompiler", "-fPIC", "-std=c++17", "-O3", "-lineinfo",
            "-gencode", "arch=compute_100a,code=sm_100a",
            "-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc")]
     if verbose:
@@ -43,8 +49,23 @@ def build(force: bool = False, verbose: bool = False) -> str:
         cmd += ["-DHARP_TM_TIMING"]
     if os.environ.get("HARP_FAST_TIMING"):        # ... and in the whole-row kernel
         cmd += ["-DHARP_FAST_TIMING"]
-    cmd += sources() + ["-o", LIB]
-    subprocess.check_call(cmd)
+    # an object a source: several at a time, and those alone whose source or headers changed
+    os.makedirs(OBJECTS, exist_ok=True)
+    headers_at = max(os.path.getmtime(p) for p in headers_of_sources())
+    flags = os.path.join(OBJECTS, "command")
+    same = os.path.exists(flags) and open(flags).read() == repr(cmd)
+
+    def compile_one(src):
+        obj = os.path.join(OBJECTS, os.path.basename(src) + ".o")
+        if force or not same or not os.path.exists(obj) or os.path.getmtime(obj) < max(headers_at, os.path.getmtime(src)):
+            subprocess.check_call(cmd + [src, "-o", obj])
+        return obj
+
+    with ThreadPoolExecutor(os.cpu_count() or 1) as pool:
+        objects = list(pool.map(compile_one, sources()))
+    with open(flags, "w") as f:
+        f.write(repr(cmd))
+    subprocess.check_call([nvcc, "-shared", "-gencode", "arch=compute_100a,code=sm_100a", *objects, "-o", LIB])
     return LIB
 
 
