@@ -321,6 +321,76 @@ harp_status_t harp_apply_host(harp_plan_t *plan, void *x_host, int64_t n_rows,
  * or a failed copy.  Synchronises with the device. */
 int32_t harp_plan_error_word(const harp_plan_t *plan);
 
+/* ---- Products of a processed layer in 8 bits, and products grouped by expert ----------------
+ * A processed weight W~ = Q_out^T W Q_in (harp_apply_two_sided) is what low-bit storage is applied to (paper, Section
+ * "Incoherence processing"); its layer is y = (x Q_in) W~^T Q_out^T.  These entry points quantise rows to 8 bits, multiply
+ * by 8-bit weights, and multiply groups of rows by a weight each (experts).  The paper fixes neither format.
+ *
+ * Matrices are row-major with a leading dimension (ld_*, in elements, at least the number of columns); weights of several
+ * groups follow one another at n rows x ld.  Buffers are aligned to their element size.  Rows (bases and leading dimensions)
+ * on 16-byte boundaries are read in place; others are copied first to scratch that the call takes on the
+ * stream from the library's pool, so weights are best kept with a padded leading dimension.  Outputs must not overlap inputs.
+ * d_in and d_out from 1 to 2^20 (8 bits: d_in to 131071, so that every sum fits 32 bits), up to 2^30 rows and 1024 groups:
+ * beyond that HARP_ERR_TOO_LARGE.  No plan is involved: pointers belong to the current device.  n_rows == 0
+ * returns HARP_OK without a launch, unless an output has to be cleared.  All are asynchronous on stream and may run on several
+ * streams at once.
+ *
+ * offsets  DEVICE int32[n_groups + 1]: group e holds rows offsets[e] <= r < offsets[e + 1], sorted, possibly none; read on the GPU.
+ *          Values are clamped to 0 .. n_rows and to the largest value before them.  Rows outside
+ *          every group are neither read for a result nor written. */
+
+/* Rows to 8 bits: a_r = max_j |x_rj|, scale_r = a_r / 127 (fp32), q_rj = 127 x_rj / a_r rounded to the nearest whole number,
+ * ties to even, as if the quotient were exact; x ~ scale q.  A row of zeros has scale 0; a row with an infinity or a NaN has
+ * scale NaN and q = 0, so that what is computed from it is NaN.  Rows of a weight give its channels' scales.
+ *   x      DEVICE n_rows x d of dtype;   q  DEVICE n_rows x d;   scale  DEVICE float[n_rows] */
+harp_status_t harp_quantize_rows(const void *x, int64_t ld_x, int64_t n_rows, int64_t d, harp_dtype_t dtype, int8_t *q,
+                                 int64_t ld_q, float *scale, void *stream);
+
+/* y_rn = x_scale_r w_scale_n sum_k x_rk w_nk: the sum exactly, in 32-bit integers; one rounding of it to fp32, one for
+ * either scale, one to y_dtype.
+ *   x  DEVICE n_rows x d_in, w  DEVICE d_out x d_in (int8);  x_scale  DEVICE float[n_rows], w_scale  DEVICE float[d_out]
+ *   y  DEVICE n_rows x d_out of y_dtype, overwritten */
+harp_status_t harp_linear_i8(const int8_t *x, int64_t ld_x, const float *x_scale, const int8_t *w, int64_t ld_w,
+                             const float *w_scale, int64_t n_rows, int64_t d_in, int64_t d_out, void *y, int64_t ld_y,
+                             harp_dtype_t y_dtype, void *stream);
+
+/* The same with a weight per group: w  DEVICE n_groups x d_out x d_in, w_scale  DEVICE float[n_groups][d_out]. */
+harp_status_t harp_grouped_linear_i8(const int8_t *x, int64_t ld_x, const float *x_scale, const int8_t *w, int64_t ld_w,
+                                     const float *w_scale, const int32_t *offsets, int32_t n_groups, int64_t n_rows,
+                                     int64_t d_in, int64_t d_out, void *y, int64_t ld_y, harp_dtype_t y_dtype, void *stream);
+
+/* y_r = x_r W_e^T for the rows of group e: x  DEVICE n_rows x d_in, w  DEVICE n_groups x d_out x d_in, both bf16;
+ * y  DEVICE n_rows x d_out of y_dtype.  Products are summed in fp32 and rounded once, in an order that the sizes fix. */
+harp_status_t harp_grouped_linear(const void *x, int64_t ld_x, const void *w, int64_t ld_w, const int32_t *offsets,
+                                  int32_t n_groups, int64_t n_rows, int64_t d_in, int64_t d_out, void *y, int64_t ld_y,
+                                  harp_dtype_t y_dtype, void *stream);
+
+/* Gradients of harp_grouped_linear for gy = dL/dy (bf16).
+ * Rows: gx_r = gy_r W_e (gx  DEVICE n_rows x d_in of gx_dtype; rows outside every group are left as they were).
+ * Weights: gw_e = sum over the rows of group e of gy_r^T x_r (gw  DEVICE n_groups x d_out x d_in of gw_dtype, overwritten, zeros
+ * for a group without rows; added to, in fp32 and rounded once, if accumulate != 0). */
+harp_status_t harp_grouped_grad_rows(const void *gy, int64_t ld_gy, const void *w, int64_t ld_w, const int32_t *offsets,
+                                     int32_t n_groups, int64_t n_rows, int64_t d_in, int64_t d_out, void *gx, int64_t ld_gx,
+                                     harp_dtype_t gx_dtype, void *stream);
+harp_status_t harp_grouped_grad_weights(const void *gy, int64_t ld_gy, const void *x, int64_t ld_x, const int32_t *offsets,
+                                        int32_t n_groups, int64_t n_rows, int64_t d_in, int64_t d_out, void *gw, int64_t ld_gw,
+                                        harp_dtype_t gw_dtype, int accumulate, void *stream);
+
+/* A processed layer in 8 bits: x <- x Q_in, its rows quantised, y = x W~^T from the 8-bit W~, y <- y Q_out^T.
+ *   x        DEVICE n_rows x dim(plan_in) of dtype, overwritten with x Q_in
+ *   w        DEVICE dim(plan_out) x dim(plan_in) int8, ld_w, with w_scale float[dim(plan_out)] (harp_quantize_rows of W~)
+ *   y        DEVICE n_rows x dim(plan_out) of dtype
+ *   scratch  DEVICE harp_processed_linear_scratch_bytes(plan_in, n_rows) bytes on a 16-byte boundary, or NULL: taken on the stream
+ * Errors of the calls it makes; both plans on the current device (else HARP_ERR_DIM_MISMATCH).  A failing call leaves x and y undefined. */
+harp_status_t harp_processed_linear_i8(const harp_plan_t *plan_in, const harp_plan_t *plan_out, void *x, int64_t n_rows,
+                                       harp_dtype_t dtype, const int8_t *w, int64_t ld_w, const float *w_scale, void *y,
+                                       void *scratch, void *stream);
+int64_t harp_processed_linear_scratch_bytes(const harp_plan_t *plan_in, int64_t n_rows);
+
+/* Wait status of the product kernels on the current device, as harp_plan_error_word is for a plan's: 0 if no wait has given
+ * up since the library was loaded.  Synchronises with the device. */
+int32_t harp_linear_error_word(void);
+
 /* Per-section cycle counters of the tensor-memory kernels and of the whole-row kernel, for profiling
  * notes.  They count only in a library built with HARP_TM_TIMING=1 / HARP_FAST_TIMING=1 in the
  * environment of the build step (clock reads at section boundaries, summed over CTAs; slot 0 = tiles);

@@ -87,6 +87,24 @@ def lib() -> ctypes.CDLL:
         L.harp_theta_device_max_radix.argtypes = []
         L.harp_plan_error_word.restype = i32
         L.harp_plan_error_word.argtypes = [vp]
+        ci = ctypes.c_int
+        L.harp_quantize_rows.restype = ci
+        L.harp_quantize_rows.argtypes = [vp, i64, i64, i64, ci, vp, i64, vp, vp]
+        L.harp_linear_i8.restype = ci
+        L.harp_linear_i8.argtypes = [vp, i64, vp, vp, i64, vp, i64, i64, i64, vp, i64, ci, vp]
+        L.harp_grouped_linear_i8.restype = ci
+        L.harp_grouped_linear_i8.argtypes = [vp, i64, vp, vp, i64, vp, vp, i32, i64, i64, i64, vp, i64, ci, vp]
+        for f in (L.harp_grouped_linear, L.harp_grouped_grad_rows):
+            f.restype = ci
+            f.argtypes = [vp, i64, vp, i64, vp, i32, i64, i64, i64, vp, i64, ci, vp]
+        L.harp_grouped_grad_weights.restype = ci
+        L.harp_grouped_grad_weights.argtypes = [vp, i64, vp, i64, vp, i32, i64, i64, i64, vp, i64, ci, ci, vp]
+        L.harp_processed_linear_i8.restype = ci
+        L.harp_processed_linear_i8.argtypes = [vp, vp, vp, i64, ci, vp, i64, vp, vp, vp, vp]
+        L.harp_processed_linear_scratch_bytes.restype = i64
+        L.harp_processed_linear_scratch_bytes.argtypes = [vp, i64]
+        L.harp_linear_error_word.restype = i32
+        L.harp_linear_error_word.argtypes = []
         L.harp_launch_count.restype = i64
         L.harp_launch_count.argtypes = []
         L.harp_status_string.restype = ctypes.c_char_p
@@ -359,6 +377,67 @@ def harp_apply_host(plan: Plan, host_ptr: int, n_rows: int, dtype: int, transpos
         raise HarpError(st, "harp_apply_host")
 
 
+# ---- products of a processed layer, by device addresses (see include/harp.h) ----
+
+def harp_quantize_rows(x_ptr: int, ld_x: int, n_rows: int, d: int, dtype: int, q_ptr: int, ld_q: int, scale_ptr: int, stream: int = 0) -> None:
+    st = lib().harp_quantize_rows(x_ptr, ld_x, n_rows, d, dtype, q_ptr, ld_q, scale_ptr, stream or None)
+    if st != HARP_OK:
+        raise HarpError(st, "harp_quantize_rows")
+
+
+def harp_linear_i8(x_ptr: int, ld_x: int, x_scale_ptr: int, w_ptr: int, ld_w: int, w_scale_ptr: int, n_rows: int, d_in: int, d_out: int,
+                   y_ptr: int, ld_y: int, y_dtype: int, stream: int = 0) -> None:
+    st = lib().harp_linear_i8(x_ptr, ld_x, x_scale_ptr, w_ptr, ld_w, w_scale_ptr, n_rows, d_in, d_out, y_ptr, ld_y, y_dtype, stream or None)
+    if st != HARP_OK:
+        raise HarpError(st, "harp_linear_i8")
+
+
+def harp_grouped_linear_i8(x_ptr: int, ld_x: int, x_scale_ptr: int, w_ptr: int, ld_w: int, w_scale_ptr: int, offsets_ptr: int, n_groups: int,
+                           n_rows: int, d_in: int, d_out: int, y_ptr: int, ld_y: int, y_dtype: int, stream: int = 0) -> None:
+    st = lib().harp_grouped_linear_i8(x_ptr, ld_x, x_scale_ptr, w_ptr, ld_w, w_scale_ptr, offsets_ptr, n_groups, n_rows, d_in, d_out,
+                                      y_ptr, ld_y, y_dtype, stream or None)
+    if st != HARP_OK:
+        raise HarpError(st, "harp_grouped_linear_i8")
+
+
+def harp_grouped_linear(x_ptr: int, ld_x: int, w_ptr: int, ld_w: int, offsets_ptr: int, n_groups: int, n_rows: int, d_in: int, d_out: int,
+                        y_ptr: int, ld_y: int, y_dtype: int, stream: int = 0) -> None:
+    st = lib().harp_grouped_linear(x_ptr, ld_x, w_ptr, ld_w, offsets_ptr, n_groups, n_rows, d_in, d_out, y_ptr, ld_y, y_dtype, stream or None)
+    if st != HARP_OK:
+        raise HarpError(st, "harp_grouped_linear")
+
+
+def harp_grouped_grad_rows(gy_ptr: int, ld_gy: int, w_ptr: int, ld_w: int, offsets_ptr: int, n_groups: int, n_rows: int, d_in: int, d_out: int,
+                           gx_ptr: int, ld_gx: int, gx_dtype: int, stream: int = 0) -> None:
+    st = lib().harp_grouped_grad_rows(gy_ptr, ld_gy, w_ptr, ld_w, offsets_ptr, n_groups, n_rows, d_in, d_out, gx_ptr, ld_gx, gx_dtype, stream or None)
+    if st != HARP_OK:
+        raise HarpError(st, "harp_grouped_grad_rows")
+
+
+def harp_grouped_grad_weights(gy_ptr: int, ld_gy: int, x_ptr: int, ld_x: int, offsets_ptr: int, n_groups: int, n_rows: int, d_in: int, d_out: int,
+                              gw_ptr: int, ld_gw: int, gw_dtype: int, accumulate: bool = False, stream: int = 0) -> None:
+    st = lib().harp_grouped_grad_weights(gy_ptr, ld_gy, x_ptr, ld_x, offsets_ptr, n_groups, n_rows, d_in, d_out, gw_ptr, ld_gw, gw_dtype,
+                                         1 if accumulate else 0, stream or None)
+    if st != HARP_OK:
+        raise HarpError(st, "harp_grouped_grad_weights")
+
+
+def harp_processed_linear_i8(plan_in: Plan, plan_out: Plan, x_ptr: int, n_rows: int, dtype: int, w_ptr: int, ld_w: int, w_scale_ptr: int,
+                             y_ptr: int, scratch_ptr: int = 0, stream: int = 0) -> None:
+    st = lib().harp_processed_linear_i8(plan_in.handle, plan_out.handle, x_ptr, n_rows, dtype, w_ptr, ld_w, w_scale_ptr, y_ptr,
+                                        scratch_ptr or None, stream or None)
+    if st != HARP_OK:
+        raise HarpError(st, "harp_processed_linear_i8")
+
+
+def harp_processed_linear_scratch_bytes(plan_in: Plan, n_rows: int) -> int:
+    return int(lib().harp_processed_linear_scratch_bytes(plan_in.handle, int(n_rows)))
+
+
+def harp_linear_error_word() -> int:
+    return int(lib().harp_linear_error_word())
+
+
 def shard_rows(n_rows: int, rank: int, world: int):
     """Contiguous row range [start, stop) of `rank` when a batch is split over `world` ranks.
     Rows are independent, so ranks need no collective on the data path."""
@@ -428,3 +507,180 @@ def two_sided_(w, plan_out: Plan, plan_in: Plan, scratch=None):
     harp_apply_two_sided(w.data_ptr(), _torch_dtype_code(w), plan_out, plan_in,
                          0 if scratch is None else scratch.data_ptr(), _raw_stream(_current_device()))
     return w
+
+
+# The products take matrices whose rows are contiguous (any row stride) on the current device, and write into `out` where it is
+# given.  What does not fit raises TypeError (dtypes) or ValueError (shapes, strides, devices) before the library is called.
+
+def _matrix(name, t, dtypes, dim, device):
+    """Leading dimension of a tensor of rows; a weight of several groups has them one behind the other."""
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name}: unsupported dtype {t.dtype}")
+    if t.dim() != dim or t.get_device() != device:
+        raise ValueError(f"{name}: {dim} dimensions on the current device expected, got {tuple(t.shape)} on {t.device}")
+    if t.is_contiguous():
+        return t.shape[-1]
+    stride = t.stride()
+    ld = stride[-2] if t.shape[-2] > 1 else max(t.shape[-1], stride[-2])
+    if (t.shape[-1] > 1 and stride[-1] != 1) or ld < t.shape[-1] or (dim == 3 and t.shape[0] > 1 and stride[0] != ld * t.shape[1]):
+        raise ValueError(f"{name}: rows have to be contiguous and evenly spaced, got strides {stride}")
+    return ld
+
+
+def _vector(name, t, dtype, n, device):
+    if t.dtype is not dtype:
+        raise TypeError(f"{name}: {dtype} expected, got {t.dtype}")
+    if t.numel() != n or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError(f"{name}: {n} contiguous values on the current device expected, got {tuple(t.shape)} on {t.device}")
+
+
+def _output(out, shape, dtype, like, device):
+    import torch
+    if out is None:
+        out = torch.empty(shape, dtype=dtype or torch.bfloat16, device=like.device)
+    elif dtype is not None and out.dtype is not dtype:
+        raise TypeError(f"out: {dtype} expected, got {out.dtype}")
+    if out.shape != shape:
+        raise ValueError(f"out: shape {tuple(shape)} expected, got {tuple(out.shape)}")
+    return out, _matrix("out", out, _dtype_codes, len(shape), device)
+
+
+def quantize_rows(x, out=None, scale=None):
+    """Rows [n, d] (fp32 or bf16) in 8 bits with a scale each: (q int8 [n, d], scale fp32 [n]), x ~ scale[:, None] * q."""
+    import torch
+    if _apply_ex is None:
+        _bind_torch()
+    device = _current_device()
+    ld_x = _matrix("x", x, _dtype_codes, 2, device)
+    n, d = x.shape
+    if out is None:
+        out = torch.empty((n, d), dtype=torch.int8, device=x.device)
+    elif out.shape != x.shape:
+        raise ValueError(f"out: shape {tuple(x.shape)} expected, got {tuple(out.shape)}")
+    ld_q = _matrix("out", out, (torch.int8,), 2, device)
+    if scale is None:
+        scale = torch.empty(n, dtype=torch.float32, device=x.device)
+    _vector("scale", scale, torch.float32, n, device)
+    harp_quantize_rows(x.data_ptr(), ld_x, n, d, _dtype_codes[x.dtype], out.data_ptr(), ld_q, scale.data_ptr(), _raw_stream(device))
+    return out, scale
+
+
+def linear_i8(x, x_scale, w, w_scale, out=None, out_dtype=None):
+    """y = (x w^T) x_scale[:, None] w_scale for int8 x [n, d_in] and w [d_out, d_in]; y is bf16 unless `out` or `out_dtype` says fp32."""
+    import torch
+    if _apply_ex is None:
+        _bind_torch()
+    device = _current_device()
+    i8 = (torch.int8,)
+    ld_x, ld_w = _matrix("x", x, i8, 2, device), _matrix("w", w, i8, 2, device)
+    (n, d_in), d_out = x.shape, w.shape[0]
+    if w.shape[1] != d_in:
+        raise ValueError(f"x has rows of {d_in} and w of {w.shape[1]}")
+    _vector("x_scale", x_scale, torch.float32, n, device)
+    _vector("w_scale", w_scale, torch.float32, d_out, device)
+    out, ld_y = _output(out, (n, d_out), out_dtype, x, device)
+    harp_linear_i8(x.data_ptr(), ld_x, x_scale.data_ptr(), w.data_ptr(), ld_w, w_scale.data_ptr(), n, d_in, d_out, out.data_ptr(), ld_y,
+                   _dtype_codes[out.dtype], _raw_stream(device))
+    return out
+
+
+def grouped_linear_i8(x, x_scale, w, w_scale, offsets, out=None, out_dtype=None):
+    """linear_i8 with a weight per group of rows: w [groups, d_out, d_in], w_scale [groups, d_out], offsets int32 [groups + 1]."""
+    import torch
+    if _apply_ex is None:
+        _bind_torch()
+    device = _current_device()
+    i8 = (torch.int8,)
+    ld_x, ld_w = _matrix("x", x, i8, 2, device), _matrix("w", w, i8, 3, device)
+    (n, d_in), (groups, d_out, d_w) = x.shape, w.shape
+    if d_w != d_in:
+        raise ValueError(f"x has rows of {d_in} and w of {d_w}")
+    _vector("x_scale", x_scale, torch.float32, n, device)
+    _vector("w_scale", w_scale, torch.float32, groups * d_out, device)
+    _vector("offsets", offsets, torch.int32, groups + 1, device)
+    out, ld_y = _output(out, (n, d_out), out_dtype, x, device)
+    harp_grouped_linear_i8(x.data_ptr(), ld_x, x_scale.data_ptr(), w.data_ptr(), ld_w, w_scale.data_ptr(), offsets.data_ptr(), groups, n, d_in,
+                           d_out, out.data_ptr(), ld_y, _dtype_codes[out.dtype], _raw_stream(device))
+    return out
+
+
+def grouped_linear(x, w, offsets, out=None, out_dtype=None):
+    """y_r = x_r w_e^T for offsets[e] <= r < offsets[e + 1]: bf16 x [n, d_in], w [groups, d_out, d_in], offsets int32 [groups + 1] on the
+    GPU; y is bf16 unless `out` or `out_dtype` says fp32.  Rows outside every group are not written."""
+    import torch
+    if _apply_ex is None:
+        _bind_torch()
+    device = _current_device()
+    bf16 = (torch.bfloat16,)
+    ld_x, ld_w = _matrix("x", x, bf16, 2, device), _matrix("w", w, bf16, 3, device)
+    (n, d_in), (groups, d_out, d_w) = x.shape, w.shape
+    if d_w != d_in:
+        raise ValueError(f"x has rows of {d_in} and w of {d_w}")
+    _vector("offsets", offsets, torch.int32, groups + 1, device)
+    out, ld_y = _output(out, (n, d_out), out_dtype, x, device)
+    harp_grouped_linear(x.data_ptr(), ld_x, w.data_ptr(), ld_w, offsets.data_ptr(), groups, n, d_in, d_out, out.data_ptr(), ld_y,
+                        _dtype_codes[out.dtype], _raw_stream(device))
+    return out
+
+
+def grouped_grad_rows(gy, w, offsets, out=None, out_dtype=None):
+    """Gradient of grouped_linear with respect to its rows: gx_r = gy_r w_e."""
+    import torch
+    if _apply_ex is None:
+        _bind_torch()
+    device = _current_device()
+    bf16 = (torch.bfloat16,)
+    ld_gy, ld_w = _matrix("gy", gy, bf16, 2, device), _matrix("w", w, bf16, 3, device)
+    (n, d_gy), (groups, d_out, d_in) = gy.shape, w.shape
+    if d_gy != d_out:
+        raise ValueError(f"gy has rows of {d_gy} and w {d_out} rows")
+    _vector("offsets", offsets, torch.int32, groups + 1, device)
+    out, ld_gx = _output(out, (n, d_in), out_dtype, gy, device)
+    harp_grouped_grad_rows(gy.data_ptr(), ld_gy, w.data_ptr(), ld_w, offsets.data_ptr(), groups, n, d_in, d_out, out.data_ptr(), ld_gx,
+                           _dtype_codes[out.dtype], _raw_stream(device))
+    return out
+
+
+def grouped_grad_weights(gy, x, offsets, out=None, out_dtype=None, accumulate=False):
+    """Gradient of grouped_linear with respect to its weights: gw_e = sum of gy_r^T x_r over the rows of e, [groups, d_out, d_in], fp32
+    unless `out` or `out_dtype` says bf16; added to `out` with accumulate."""
+    import torch
+    if _apply_ex is None:
+        _bind_torch()
+    device = _current_device()
+    bf16 = (torch.bfloat16,)
+    ld_gy, ld_x = _matrix("gy", gy, bf16, 2, device), _matrix("x", x, bf16, 2, device)
+    (n, d_out), (n_x, d_in), groups = gy.shape, x.shape, offsets.numel() - 1
+    if n != n_x:
+        raise ValueError(f"gy has {n} rows and x {n_x}")
+    if accumulate and out is None:
+        raise ValueError("accumulate needs out")
+    _vector("offsets", offsets, torch.int32, groups + 1, device)
+    out, ld_gw = _output(out, (groups, d_out, d_in), out_dtype or (torch.float32 if out is None else None), gy, device)
+    harp_grouped_grad_weights(gy.data_ptr(), ld_gy, x.data_ptr(), ld_x, offsets.data_ptr(), groups, n, d_in, d_out, out.data_ptr(), ld_gw,
+                              _dtype_codes[out.dtype], accumulate, _raw_stream(device))
+    return out
+
+
+def processed_linear_i8(x, plan_in: Plan, plan_out: Plan, w, w_scale, out=None, scratch=None):
+    """A processed layer in 8 bits, y = (x Q_in) W~^T Q_out^T: contiguous rows x [n, plan_in.d] (fp32 or bf16; overwritten with x Q_in), W~ as
+    quantize_rows gave it.  `scratch`: contiguous, harp_processed_linear_scratch_bytes(plan_in, n) bytes at least."""
+    import torch
+    if _apply_ex is None:
+        _bind_torch()
+    device = _current_device()
+    _matrix("x", x, _dtype_codes, 2, device)
+    ld_w = _matrix("w", w, (torch.int8,), 2, device)
+    n = x.shape[0]
+    if not x.is_contiguous() or x.shape[1] != plan_in.d or w.shape != (plan_out.d, plan_in.d):
+        raise ValueError(f"contiguous rows of {plan_in.d} and a weight {(plan_out.d, plan_in.d)} expected, got {tuple(x.shape)} and {tuple(w.shape)}")
+    _vector("w_scale", w_scale, torch.float32, plan_out.d, device)
+    out, _ = _output(out, (n, plan_out.d), x.dtype, x, device)
+    if not out.is_contiguous():
+        raise ValueError("out has to be contiguous")
+    if scratch is not None and (not scratch.is_contiguous() or scratch.get_device() != device or
+                                scratch.numel() * scratch.element_size() < harp_processed_linear_scratch_bytes(plan_in, n)):
+        raise ValueError(f"scratch of {harp_processed_linear_scratch_bytes(plan_in, n)} bytes on the current device expected")
+    harp_processed_linear_i8(plan_in, plan_out, x.data_ptr(), n, _dtype_codes[x.dtype], w.data_ptr(), ld_w, w_scale.data_ptr(), out.data_ptr(),
+                             0 if scratch is None else scratch.data_ptr(), _raw_stream(device))
+    return out

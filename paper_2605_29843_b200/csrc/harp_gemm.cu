@@ -1,0 +1,552 @@
+// Products of a layer on the tensor cores (tcgen05.mma, operands and accumulators fed by bulk tensor copies):
+//
+//   FORWARD        y[r][n]  = sum_k x[r][k] w_e[n][k]       (8 bits: times row_scale[r] channel_scale_e[n])
+//   GRAD_ROWS      dx[r][k] = sum_n dy[r][n] w_e[n][k]
+//   GRAD_WEIGHTS   dw_e[n][k] = sum_{r in e} dy[r][n] x[r][k]
+//
+// e: the group that row r belongs to.  In all three the dimension that is contiguous in the output lies along the lanes of
+// tensor memory and the other one along its columns.  A warp then stores 32 neighbouring elements of an output row, and
+// the number of columns of an instruction follows the rows that a group has (N = 16, 32, ... 256), so that a group of 40
+// rows costs the products of 64 and no more.
+//
+// Two CTAs of a cluster work on one tile of 256 lanes x up to 256 columns (cta_group::2: either holds half of both
+// operands, 32 KB a stage of 128 bytes along the contracted dimension) or, where that leaves SMs idle, a CTA works on 128 x 128 and up to
+// eight of them divide the contracted dimension and add up their accumulators through distributed shared memory, in the
+// order of their ranks.  Tiles are handed out round robin; the accumulators of two tiles fit tensor memory, so a tile's
+// epilogue runs under the next one's products.
+//
+// Every operand is brought by tiled copies with the 128-byte swizzle, K-major where the contracted dimension is contiguous and
+// MN-major where it is not (w in GRAD_ROWS, both operands in GRAD_WEIGHTS: no transposed copy of anything is made).  Copies
+// past the end of a matrix fill zeros.  Past the end of a group they bring the next group's rows: harmless columns where rows lie
+// along the columns; in GRAD_WEIGHTS a warp overwrites them with zeros before the products, in both
+// operands, because the other group's values may be infinite.
+#include <algorithm>
+#include <mutex>
+
+#include <cuda.h>
+
+#include "harp_gemm_ptx.cuh"
+#include "harp_internal.h"
+#include "harp_linear.h"
+
+namespace harp_linear {
+namespace {
+
+using namespace harp_gemm_ptx;
+
+constexpr int kThreads = 256;                // warps: 0 copies, 1 products, 2 tensor memory and ragged ends, 3 offsets, 4-7 epilogue
+constexpr int kHalf = 16384;                 // one operand's part of a stage in one CTA
+constexpr int kStage = 2 * kHalf;
+constexpr int kMaxStages = 6;
+constexpr uint32_t kSpin = 1u << 22;         // limit of every wait
+
+__device__ int32_t g_gemm_err;
+
+struct Params {
+    int32_t lanes, cols, depth;              // cols: of GRAD_WEIGHTS alone; depth: of the others
+    int32_t n_rows, n_groups;
+    const int32_t *offsets;
+    int32_t tile_cols, box_rows;             // most columns of a tile; rows that a copy of the column operand brings
+    int32_t split, stages;                   // CTAs that divide the contracted dimension
+    void *out;
+    int64_t ld_out, group_out;               // group_out: elements between two groups' outputs (GRAD_WEIGHTS)
+    const float *row_scale, *channel_scale;
+    int32_t accumulate;
+    int32_t *err;
+};
+
+struct Tile {
+    int e, lane0, col0, cols, row0, blocks, tail;    // cols: valid ones; row0: first row; tail: rows in the last block (GRAD_WEIGHTS)
+};
+
+__device__ __forceinline__ int div_up(int a, int b) { return (a + b - 1) / b; }
+__device__ __forceinline__ int round_up(int a, int b) { return div_up(a, b) * b; }
+
+// columns of the tiles of a group of n rows: as even as the instruction's sizes let them be
+template <int CG>
+__device__ __forceinline__ int even_cols(int n, int most) {
+    return n <= 0 ? most : round_up(div_up(n, div_up(n, most)), CG == 2 ? 32 : 16);
+}
+
+// Which tile is number t.  Neighbouring numbers share operands: bands of eight lane tiles, column tiles along a band.
+template <int CG, int PRODUCT, int BLOCK>
+__device__ __forceinline__ Tile tile_at(int t, const Params &P, const int *off, const int *first) {
+    Tile T;
+    const int lane_tiles = div_up(P.lanes, 128 * CG);
+    int idx, col_tiles, tc;
+    if (PRODUCT == GRAD_WEIGHTS) {
+        col_tiles = div_up(P.cols, P.tile_cols);
+        tc = P.tile_cols;
+        T.e = t / (lane_tiles * col_tiles);
+        idx = t - T.e * (lane_tiles * col_tiles);
+    } else {
+        int lo = 0, hi = P.n_groups;             // the last group whose first tile is at or below t
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (first[mid] <= t) lo = mid;
+            else hi = mid;
+        }
+        T.e = lo;
+        idx = t - first[lo];
+        tc = even_cols<CG>(off[lo + 1] - off[lo], P.tile_cols);
+        col_tiles = div_up(off[lo + 1] - off[lo], tc);
+    }
+    const int band = idx / (8 * col_tiles), in_band = idx - band * 8 * col_tiles;
+    const int width = min(8, lane_tiles - band * 8);
+    T.lane0 = (band * 8 + in_band % width) * 128 * CG;
+    T.col0 = (in_band / width) * tc;
+    const int n = off[T.e + 1] - off[T.e];
+    if (PRODUCT == GRAD_WEIGHTS) {
+        T.cols = min(tc, P.cols - T.col0);
+        T.row0 = off[T.e];
+        T.blocks = div_up(n, BLOCK);
+        T.tail = n - (T.blocks - 1) * BLOCK;
+    } else {
+        T.cols = min(tc, n - T.col0);
+        T.row0 = off[T.e] + T.col0;
+        T.blocks = div_up(P.depth, BLOCK);
+        T.tail = BLOCK;
+    }
+    return T;
+}
+
+struct Waiter {
+    volatile int *dead;
+    int32_t *err;
+    // false when the wait gave up (here or elsewhere in the CTA)
+    __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity, int code) const {
+        for (uint32_t it = 0; it < kSpin; ++it) {
+            if (mbar_try_cluster(bar, parity)) return true;
+            if ((it & 63) == 63 && *dead) return false;
+        }
+        *dead = 1;
+        atomicExch(err, code);
+        return false;
+    }
+};
+
+__device__ __forceinline__ void store(float *p, float v) { *p = v; }
+__device__ __forceinline__ void store(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
+__device__ __forceinline__ float load(const float *p) { return *p; }
+__device__ __forceinline__ float load(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
+
+template <bool I8, int CG, int PRODUCT, typename Out>
+__global__ void __launch_bounds__(kThreads, 1)
+harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const Params P) {
+    constexpr int BLOCK = I8 ? 128 : 64;                     // contracted elements a stage
+    constexpr bool A_MN = PRODUCT != FORWARD, B_MN = PRODUCT == GRAD_WEIGHTS;
+    constexpr uint32_t COLUMNS = CG == 2 ? 512 : 256;        // two accumulators
+    constexpr uint32_t ACC = COLUMNS / 2;
+
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t bars[3 * kMaxStages + 6];
+    __shared__ uint32_t s_columns;
+    __shared__ int s_dead;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();                    // 0 without a cluster
+    const int size = CG == 2 ? 2 : P.split;                  // CTAs a cluster
+    const int cluster = blockIdx.x / size, clusters = gridDim.x / size;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    unsigned char *const base_ptr = smem_raw + (base - smem_u32(smem_raw));
+    const uint32_t sums = base + (uint32_t)P.stages * kStage;        // the other ranks' accumulators (split > 1)
+    int *const off = reinterpret_cast<int *>(base_ptr + P.stages * kStage + (P.split > 1 ? P.tile_cols * 512 : 0));
+    int *const first = off + P.n_groups + 1;
+
+    const uint32_t bar0 = smem_u32(bars);
+    auto full = [&](int s) { return bar0 + 8u * s; };                            // a stage has arrived
+    auto empty = [&](int s) { return bar0 + 8u * (kMaxStages + s); };            // a stage has been multiplied
+    auto ready = [&](int s) { return bar0 + 8u * (2 * kMaxStages + s); };        // ... is free of other groups' rows in both CTAs (GRAD_WEIGHTS)
+    auto done = [&](int a) { return bar0 + 8u * (3 * kMaxStages + a); };         // an accumulator is complete
+    auto taken = [&](int a) { return bar0 + 8u * (3 * kMaxStages + 2 + a); };    // ... has been read
+    const uint32_t sums_full = bar0 + 8u * (3 * kMaxStages + 4), sums_free = bar0 + 8u * (3 * kMaxStages + 5);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kMaxStages; ++s) {
+            mbar_init(full(s), 1);
+            mbar_init(empty(s), 1);
+            mbar_init(ready(s), CG);
+        }
+        for (int a = 0; a < 2; ++a) {
+            mbar_init(done(a), 1);
+            mbar_init(taken(a), 4 * CG);
+        }
+        mbar_init(sums_full, 4 * P.split);
+        mbar_init(sums_free, 4 * P.split);
+        mbar_init_fence();
+        s_dead = 0;
+        prefetch_map(&map_a);
+        prefetch_map(&map_b);
+    }
+    if (warp == 2) alloc_columns<CG>(smem_u32(&s_columns), COLUMNS);
+    wait_for_previous();
+    launch_dependents();
+    if (warp == 3) {
+        // offsets made to rise and to stay within the batch, and the number of tiles before each group
+        int before = 0, tiles = 0;
+        for (int e0 = 0; e0 <= P.n_groups; e0 += 32) {
+            const int e = e0 + lane;
+            int o = P.offsets == nullptr ? (e == 0 ? 0 : P.n_rows) : e <= P.n_groups ? P.offsets[e] : P.n_rows;
+            o = min(max(o, 0), P.n_rows);
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int v = __shfl_up_sync(~0u, o, d);
+                if (lane >= d) o = max(o, v);
+            }
+            o = max(o, before);
+            int prev = __shfl_up_sync(~0u, o, 1);
+            if (lane == 0) prev = before;
+            int n = 0;                                        // tiles of group e - 1
+            if (e > 0 && e <= P.n_groups && PRODUCT != GRAD_WEIGHTS && o > prev)
+                n = div_up(P.lanes, 128 * CG) * div_up(o - prev, even_cols<CG>(o - prev, P.tile_cols));
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int v = __shfl_up_sync(~0u, n, d);
+                if (lane >= d) n += v;
+            }
+            if (e <= P.n_groups) {
+                off[e] = o;
+                first[e] = tiles + n;
+            }
+            before = __shfl_sync(~0u, o, 31);
+            tiles += __shfl_sync(~0u, n, 31);
+        }
+    }
+    tc_fence_before();
+    if (size > 1) cluster_sync();
+    else __syncthreads();
+    tc_fence_after();
+
+    const uint32_t columns = s_columns;
+    const Waiter wait{&s_dead, P.err};
+    const int n_tiles = PRODUCT == GRAD_WEIGHTS ? P.n_groups * div_up(P.lanes, 128 * CG) * div_up(P.cols, P.tile_cols) : first[P.n_groups];
+    auto at = [&](int t) { return tile_at<CG, PRODUCT, BLOCK>(t, P, off, first); };
+    // this CTA's share of the blocks
+    auto from = [&](const Tile &T) { return CG == 2 ? 0 : (int)((int64_t)T.blocks * (int)rank / P.split); };
+    auto to = [&](const Tile &T) { return CG == 2 ? T.blocks : (int)((int64_t)T.blocks * ((int)rank + 1) / P.split); };
+    auto width = [&](const Tile &T) { return round_up(T.cols, CG == 2 ? 32 : 16); };     // columns of the instruction
+
+    if (warp == 0 && lane == 0) {
+        int it = 0;
+        bool alive = true;
+        for (int t = cluster; alive && t < n_tiles; t += clusters) {
+            const Tile T = at(t);
+            const int half = width(T) / CG;                  // columns of this CTA
+            const int lane0 = T.lane0 + (CG == 2 ? (int)rank * 128 : 0), col0 = (int)rank * (CG == 2 ? half : 0);
+            const int boxes = B_MN ? div_up(half, 64) : div_up(half, P.box_rows);
+            const uint32_t box_bytes = B_MN ? 8192u : (uint32_t)P.box_rows * 128u;
+            const uint32_t bytes = kHalf + (uint32_t)boxes * box_bytes;
+            for (int b = from(T); b < to(T); ++b, ++it) {
+                const int s = it % P.stages;
+                if (!wait(empty(s), ((it / P.stages) & 1) ^ 1, 1)) { alive = false; break; }
+                const uint32_t a = base + (uint32_t)s * kStage, bb = a + kHalf;
+                uint32_t bar = full(s);
+                if (CG == 2 && PRODUCT != GRAD_WEIGHTS) {    // one barrier, the first CTA's, for both halves
+                    if (rank == 0) mbar_expect_tx(bar, 2 * bytes);
+                    else bar = map_rank(bar, 0);
+                } else mbar_expect_tx(bar, bytes);
+                const int k = b * BLOCK;
+                if (PRODUCT == FORWARD) load_3d<CG>(a, &map_a, k, lane0, T.e, bar);
+                else if (PRODUCT == GRAD_ROWS) {
+                    load_3d<CG>(a, &map_a, lane0, k, T.e, bar);
+                    load_3d<CG>(a + 8192, &map_a, lane0 + 64, k, T.e, bar);
+                } else {
+                    tma_load_2d(a, &map_a, lane0, T.row0 + k, bar);
+                    tma_load_2d(a + 8192, &map_a, lane0 + 64, T.row0 + k, bar);
+                }
+                for (int i = 0; i < boxes; ++i) {
+                    if (B_MN) tma_load_2d(bb + i * 8192, &map_b, T.col0 + col0 + i * 64, T.row0 + k, bar);
+                    else load_2d<CG>(bb + i * box_bytes, &map_b, k, T.row0 + col0 + i * P.box_rows, bar);
+                }
+            }
+        }
+        if (!alive && (rank == 0 || CG == 1 || PRODUCT == GRAD_WEIGHTS))
+            // leave no copy in flight: the last use of every stage, as far as there was one
+            for (int s = 0; s < P.stages && s < it; ++s) {
+                const int use = (it - 1 - s) / P.stages;
+                for (uint32_t i = 0; i < kSpin && !mbar_try(full(s), use & 1); ++i) {}
+            }
+    } else if (warp == 1 && lane == 0 && (CG == 1 || rank == 0)) {
+        int it = 0, n = 0;
+        bool alive = true;
+        for (int t = cluster; alive && t < n_tiles; t += clusters) {
+            const Tile T = at(t);
+            const int b0 = from(T), b1 = to(T);
+            if (T.blocks == 0) continue;
+            const uint32_t idesc = instr(I8, A_MN, B_MN, 128 * CG, width(T));
+            const int acc = n & 1;
+            if (!wait(taken(acc), ((n >> 1) & 1) ^ 1, 2)) break;
+            tc_fence_after();
+            const uint32_t d = columns + acc * ACC;
+            for (int b = b0; b < b1; ++b, ++it) {
+                const int s = it % P.stages;
+                if (!wait(PRODUCT == GRAD_WEIGHTS ? ready(s) : full(s), (it / P.stages) & 1, 3)) { alive = false; break; }
+                tc_fence_after();
+                const uint32_t a = base + (uint32_t)s * kStage;
+                const uint64_t da = A_MN ? operand(a, 8192, 1024) : operand(a, 16, 1024);
+                const uint64_t db = B_MN ? operand(a + kHalf, 8192, 1024) : operand(a + kHalf, 16, 1024);
+                const int steps = PRODUCT == GRAD_WEIGHTS && b == T.blocks - 1 ? div_up(T.tail, 16) : 4;
+                for (int k = 0; k < steps; ++k)
+                    mma_ss<I8, CG>(d, da + (uint64_t)(A_MN ? 128 : 2) * k, db + (uint64_t)(B_MN ? 128 : 2) * k, idesc, b > b0 || k > 0);
+                commit<CG>(empty(s));
+            }
+            if (alive && b1 > b0) commit<CG>(done(acc));
+            ++n;
+        }
+    } else if (warp == 2 && PRODUCT == GRAD_WEIGHTS) {
+        int it = 0;
+        bool alive = true;
+        for (int t = cluster; alive && t < n_tiles; t += clusters) {
+            const Tile T = at(t);
+            const int chunks = 2 + div_up(width(T) / CG, 64);        // of 64 lanes or columns, 64 rows of 128 bytes each
+            for (int b = 0; b < T.blocks; ++b, ++it) {
+                const int s = it % P.stages;
+                if (!wait(full(s), (it / P.stages) & 1, 4)) { alive = false; break; }
+                if (b == T.blocks - 1 && T.tail % 16) {
+                    for (int c = 0; c < chunks; ++c)
+                        for (int r = T.tail; r < round_up(T.tail, 16); ++r)
+                            *reinterpret_cast<uint32_t *>(base_ptr + s * kStage + c * 8192 + r * 128 + lane * 4) = 0;
+                    fence_async_smem();
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(CG == 2 ? map_rank(ready(s), 0) : ready(s));
+            }
+        }
+    } else if (warp >= 4) {
+        const int q = warp - 4;
+        int n = 0;
+        bool alive = true;
+        for (int t = cluster; alive && t < n_tiles; t += clusters) {
+            const Tile T = at(t);
+            const int l = T.lane0 + (CG == 2 ? (int)rank * 128 : 0) + q * 32 + lane;
+            const bool inside = l < P.lanes;
+            Out *const out = static_cast<Out *>(P.out) +
+                (PRODUCT == GRAD_WEIGHTS ? T.e * P.group_out + (int64_t)T.col0 * P.ld_out : (int64_t)T.row0 * P.ld_out) + l;
+            const float by_lane = I8 && inside ? P.channel_scale[(int64_t)T.e * P.lanes + l] : 1.0f;
+            auto put = [&](int c, float v) {
+                if (PRODUCT == GRAD_WEIGHTS && P.accumulate) v += load(out + (int64_t)c * P.ld_out);
+                store(out + (int64_t)c * P.ld_out, v);
+            };
+            if (T.blocks == 0) {                             // a group without rows
+                if (inside && !P.accumulate)
+                    for (int c = 0; c < T.cols; ++c) store(out + (int64_t)c * P.ld_out, 0.0f);
+                continue;
+            }
+            const int acc = n & 1;
+            const bool any = to(T) > from(T);
+            if (any && !wait(done(acc), (n >> 1) & 1, 5)) break;
+            tc_fence_after();
+            const uint32_t d = columns + acc * ACC + ((uint32_t)q << 21);
+            const int w = width(T);
+            if (P.split == 1) {
+                for (int c0 = 0; c0 < w; c0 += 16) {
+                    uint32_t v[16];
+                    tmem_ld16(d + c0, v);
+                    tmem_wait_ld();
+                    if (inside) {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j)
+                            if (c0 + j < T.cols) {
+                                const float x = I8 ? (float)(int32_t)v[j] * by_lane * P.row_scale[T.row0 + c0 + j] : __uint_as_float(v[j]);
+                                put(c0 + j, x);
+                            }
+                    }
+                }
+            } else {
+                // columns dealt out to the ranks in runs of `run`; sums[source][column of the run][lane]
+                const int run = div_up(w, P.split);
+                if (!wait(sums_free, (n & 1) ^ 1, 6)) { alive = false; break; }
+                for (int c0 = 0; c0 < w; c0 += 16) {
+                    uint32_t v[16];
+                    if (any) {
+                        tmem_ld16(d + c0, v);
+                        tmem_wait_ld();
+                    }
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (c0 + j < T.cols) {
+                            const int to_rank = (c0 + j) / run, c = (c0 + j) - to_rank * run;
+                            st_cluster(map_rank(sums + (uint32_t)(((int)rank * run + c) * 128 + q * 32 + lane) * 4, to_rank), any ? v[j] : 0u);
+                        }
+                }
+                __syncwarp();
+                if (lane < P.split) mbar_arrive_cluster(map_rank(sums_full, lane));
+                if (!wait(sums_full, n & 1, 7)) { alive = false; break; }
+                const uint32_t *const mine = reinterpret_cast<const uint32_t *>(base_ptr + P.stages * kStage) + q * 32 + lane;
+                for (int c = 0; c < run; ++c) {
+                    const int col = (int)rank * run + c;
+                    if (col >= T.cols) break;
+                    float x;
+                    if (I8) {
+                        int32_t sum = 0;
+                        for (int r = 0; r < P.split; ++r) sum += (int32_t)mine[(r * run + c) * 128];
+                        x = (float)sum * by_lane * P.row_scale[T.row0 + col];
+                    } else {
+                        x = 0.0f;
+                        for (int r = 0; r < P.split; ++r) x += __uint_as_float(mine[(r * run + c) * 128]);
+                    }
+                    if (inside) put(col, x);
+                }
+                __syncwarp();
+                if (lane < P.split) mbar_arrive_cluster(map_rank(sums_free, lane));
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(CG == 2 ? map_rank(taken(acc), 0) : taken(acc));
+            ++n;
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    if (size > 1) cluster_sync();                            // the others' barriers and memory stay until all are done
+    else __syncthreads();
+    if (warp == 2) {
+        tc_fence_after();
+        free_columns<CG>(columns, COLUMNS);
+    }
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                  const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+bool encode(CUtensorMap *map, bool i8, const void *ptr, int rank, const int64_t *extent, const int64_t *pitch, const int *box) {
+    cuuint64_t dims[3], strides[2];
+    cuuint32_t b[3], ones[3] = {1, 1, 1};
+    for (int i = 0; i < rank; ++i) {
+        dims[i] = (cuuint64_t)extent[i];
+        b[i] = (cuuint32_t)box[i];
+        if (i + 1 < rank) strides[i] = (cuuint64_t)pitch[i];
+    }
+    return reinterpret_cast<EncodeTiledFn>(harp_tensor_map_encoder(nullptr))(
+               map, i8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void *>(ptr), dims,
+               strides, b, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int smem_bytes(const Params &P) {
+    return 1024 + P.stages * kStage + (P.split > 1 ? P.tile_cols * 512 : 0) + 8 * (P.n_groups + 1);
+}
+
+template <bool I8, int CG, int PRODUCT, typename Out>
+harp_status_t launch(const CUtensorMap &a, const CUtensorMap &b, const Params &P, int clusters, cudaStream_t s) {
+    const auto kernel = harp_gemm_kernel<I8, CG, PRODUCT, Out>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448 - 1024) != cudaSuccess) return HARP_ERR_CUDA;
+    const int size = CG == 2 ? 2 : P.split;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(clusters * size));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = (size_t)smem_bytes(P);
+    cfg.stream = s;
+    cudaLaunchAttribute la[2];
+    la[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    la[0].val.programmaticStreamSerializationAllowed = 1;
+    la[1].id = cudaLaunchAttributeClusterDimension;
+    la[1].val.clusterDim.x = (unsigned)size;
+    la[1].val.clusterDim.y = la[1].val.clusterDim.z = 1;
+    cfg.attrs = la;
+    cfg.numAttrs = 2;
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, kernel, a, b, P);
+    g_harp_launches.fetch_add(1, std::memory_order_relaxed);
+    if (err != cudaSuccess) {
+        cudaGetLastError();
+        return HARP_ERR_CUDA;
+    }
+    return HARP_OK;
+}
+
+template <bool I8, int CG, int PRODUCT>
+harp_status_t launch(harp_dtype_t out, const CUtensorMap &a, const CUtensorMap &b, const Params &P, int clusters, cudaStream_t s) {
+    return out == HARP_F32 ? launch<I8, CG, PRODUCT, float>(a, b, P, clusters, s) : launch<I8, CG, PRODUCT, __nv_bfloat16>(a, b, P, clusters, s);
+}
+
+}  // namespace
+
+const Device *device() {
+    constexpr int kMost = 64;
+    static Device table[kMost];
+    static std::once_flag once[kMost];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMost) return nullptr;
+    std::call_once(once[dev], [dev] {
+        Device d;
+        void *err = nullptr;
+        if (!harp_tensor_map_encoder(nullptr) || cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+            cudaGetSymbolAddress(&err, g_gemm_err) != cudaSuccess) {
+            cudaGetLastError();
+            return;
+        }
+        d.err = static_cast<int32_t *>(err);
+        const auto kernel = harp_gemm_kernel<false, 2, FORWARD, __nv_bfloat16>;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)d.sms / 2 * 2);
+        cfg.blockDim = dim3(kThreads);
+        cfg.dynamicSmemBytes = 1024 + kMaxStages * kStage + 8 * (kMaxGroups + 1);
+        cudaLaunchAttribute la;
+        la.id = cudaLaunchAttributeClusterDimension;
+        la.val.clusterDim.x = 2;
+        la.val.clusterDim.y = la.val.clusterDim.z = 1;
+        cfg.attrs = &la;
+        cfg.numAttrs = 1;
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448 - 1024) != cudaSuccess ||
+            cudaOccupancyMaxActiveClusters(&d.pairs, kernel, &cfg) != cudaSuccess || d.pairs < 1) {
+            cudaGetLastError();
+            return;
+        }
+        table[dev] = d;
+    });
+    return table[dev].err ? &table[dev] : nullptr;
+}
+
+harp_status_t gemm(const Call &c, const Device &dev, cudaStream_t stream) {
+    const int es = c.i8 ? 1 : 2;
+    Params P = {};
+    P.n_rows = (int32_t)c.n_rows;
+    P.n_groups = c.n_groups;
+    P.offsets = c.offsets;
+    P.row_scale = c.row_scale;
+    P.channel_scale = c.channel_scale;
+    P.out = c.out;
+    P.ld_out = c.ld_out;
+    P.group_out = c.d_out * c.ld_out;
+    P.accumulate = c.accumulate;
+    P.err = dev.err;
+    P.lanes = (int32_t)(c.product == FORWARD ? c.d_out : c.d_in);
+    P.cols = (int32_t)c.d_out;
+    P.depth = (int32_t)(c.product == FORWARD ? c.d_in : c.d_out);
+    P.tile_cols = 256;
+    P.stages = kMaxStages;
+    P.split = 1;
+    int cg = 2;
+    int64_t tiles;
+    if (c.product == GRAD_WEIGHTS) {
+        tiles = (int64_t)c.n_groups * ((P.lanes + 255) / 256) * ((P.cols + 255) / 256);
+    } else {
+        tiles = ((int64_t)P.lanes + 255) / 256 * ((c.n_rows + 255) / 256 + c.n_groups - 1);
+        P.box_rows = 32;
+    }
+    if (tiles > INT32_MAX / 2) return HARP_ERR_TOO_LARGE;
+    const int clusters = (int)std::min<int64_t>(tiles, cg == 2 ? dev.pairs : dev.sms / P.split);
+
+    CUtensorMap a, b;
+    const int elems = 128 / es;
+    bool ok;
+    if (c.product == GRAD_WEIGHTS) {
+        const int64_t ea[2] = {c.d_in, c.n_rows}, pa[1] = {c.ld_rows * es}, eb[2] = {c.d_out, c.n_rows}, pb[1] = {c.ld_other * es};
+        const int box[2] = {64, 64};
+        ok = encode(&a, false, c.rows, 2, ea, pa, box) && encode(&b, false, c.other, 2, eb, pb, box);
+    } else {
+        const int64_t ea[3] = {c.d_in, c.d_out, c.n_groups}, pa[2] = {c.ld_other * es, c.ld_other * es * c.d_out};
+        const int box_a[3] = {elems, c.product == FORWARD ? 128 : 64, 1};
+        const int64_t eb[2] = {c.d_rows, c.n_rows}, pb[1] = {c.ld_rows * es};
+        const int box_b[2] = {elems, P.box_rows};
+        ok = encode(&a, c.i8, c.other, 3, ea, pa, box_a) && encode(&b, c.i8, c.rows, 2, eb, pb, box_b);
+    }
+    if (!ok) return HARP_ERR_UNSUPPORTED;
+    if (c.i8) return launch<true, 2, FORWARD>(c.out_dtype, a, b, P, clusters, stream);
+    if (c.product == FORWARD) return launch<false, 2, FORWARD>(c.out_dtype, a, b, P, clusters, stream);
+    if (c.product == GRAD_ROWS) return launch<false, 2, GRAD_ROWS>(c.out_dtype, a, b, P, clusters, stream);
+    return launch<false, 2, GRAD_WEIGHTS>(c.out_dtype, a, b, P, clusters, stream);
+}
+
+}  // namespace harp_linear

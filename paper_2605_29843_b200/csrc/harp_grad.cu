@@ -1762,6 +1762,8 @@ harp_status_t grad_blocks(const harp_plan *plan, const T *x, const T *gy, int64_
 
 }  // namespace
 
+cudaMemPool_t harp_scratch_pool(int device) { return scratch_pool(device); }
+
 extern "C" int64_t harp_plan_n_params(const harp_plan_t *plan) { return plan ? plan->n_params : -1; }
 
 extern "C" harp_status_t harp_grad_blocks(const harp_plan_t *plan, const void *x, const void *gy, int64_t n_rows,

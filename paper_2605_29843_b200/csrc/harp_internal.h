@@ -100,7 +100,7 @@ harp_status_t harp_tm_build(harp_plan *plan);
 void harp_tm_destroy(harp_plan *plan);
 harp_status_t harp_tm_apply(const harp_plan *plan, void *x, int64_t n_rows, harp_dtype_t dtype,
                             int transpose, cudaStream_t stream);
-// cuTensorMapEncodeTiled of the driver (null if it has none, or for a plan built without: HARP_NO_TENSOR_MAPS)
+// cuTensorMapEncodeTiled of the driver (null if it has none, or for a plan built without: HARP_NO_TENSOR_MAPS); the plan may be null
 void *harp_tensor_map_encoder(const harp_plan *plan);
 int32_t harp_tm_error_word(const harp_plan *plan);
 // the stages below stride 256 alone (lower pass of the two-pass paths); 0 stages = not available
@@ -127,6 +127,9 @@ harp_status_t harp_f32_apply(const harp_plan *plan, void *x, int64_t n_rows, har
                              cudaStream_t stream);
 harp_status_t harp_f32_col_apply(const harp_plan *plan, void *W, int64_t n_cols, int64_t ld, harp_dtype_t dtype,
                                  cudaStream_t stream);
+
+// memory pool of the library's own on this device, from which calls take scratch (harp_grad.cu); null if there is none
+cudaMemPool_t harp_scratch_pool(int device);
 
 // out-of-place matrix transpose, rows x cols -> cols x rows (harp_two_sided.cu)
 harp_status_t harp_transpose_matrix(const void *src, void *dst, int64_t rows, int64_t cols,

@@ -742,7 +742,7 @@ namespace {
 
 }  // namespace
 
-void *harp_tensor_map_encoder(const harp_plan *plan) { return plan->opt_no_maps ? nullptr : reinterpret_cast<void *>(encode_fn()); }
+void *harp_tensor_map_encoder(const harp_plan *plan) { return plan && plan->opt_no_maps ? nullptr : reinterpret_cast<void *>(encode_fn()); }
 
 namespace {
 
