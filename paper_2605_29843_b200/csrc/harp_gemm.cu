@@ -37,7 +37,6 @@ using namespace harp_gemm_ptx;
 constexpr int kThreads = 256;                // warps: 0 copies, 1 products, 2 tensor memory and ragged ends, 3 offsets, 4-7 epilogue
 constexpr int kHalf = 16384;                 // one operand's part of a stage in one CTA
 constexpr int kStage = 2 * kHalf;
-constexpr int kMaxStages = 6;
 constexpr uint32_t kSpin = 1u << 22;         // limit of every wait
 
 __device__ int32_t g_gemm_err;
@@ -46,8 +45,8 @@ struct Params {
     int32_t lanes, cols, depth;              // cols: of GRAD_WEIGHTS alone; depth: of the others
     int32_t n_rows, n_groups;
     const int32_t *offsets;
-    int32_t tile_cols, box_rows;             // most columns of a tile; rows that a copy of the column operand brings
-    int32_t split, stages;                   // CTAs that divide the contracted dimension
+    int32_t tile_cols;                       // most columns of a tile
+    int32_t split;                           // CTAs that divide the contracted dimension
     void *out;
     int64_t ld_out, group_out;               // group_out: elements between two groups' outputs (GRAD_WEIGHTS)
     const float *row_scale, *channel_scale;
@@ -114,15 +113,18 @@ struct Waiter {
     volatile int *dead;
     int32_t *err;
     // false when the wait gave up (here or elsewhere in the CTA)
+    template <bool CLUSTER = false>
     __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity, int code) const {
         for (uint32_t it = 0; it < kSpin; ++it) {
-            if (mbar_try_cluster(bar, parity)) return true;
+            if (CLUSTER ? mbar_try_cluster(bar, parity) : mbar_try(bar, parity)) return true;
             if ((it & 63) == 63 && *dead) return false;
         }
         *dead = 1;
         atomicExch(err, code);
         return false;
     }
+    // behind stores of another CTA
+    __device__ __forceinline__ bool cluster(uint32_t bar, uint32_t parity, int code) const { return operator()<true>(bar, parity, code); }
 };
 
 __device__ __forceinline__ void store(float *p, float v) { *p = v; }
@@ -130,16 +132,36 @@ __device__ __forceinline__ void store(__nv_bfloat16 *p, float v) { *p = __float2
 __device__ __forceinline__ float load(const float *p) { return *p; }
 __device__ __forceinline__ float load(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
 
+// stage and phase of the ring of stages
+template <int STAGES>
+struct Ring {
+    int s = 0;
+    uint32_t phase = 0;
+    __device__ __forceinline__ void next() {
+        if (++s == STAGES) {
+            s = 0;
+            phase ^= 1;
+        }
+    }
+    __device__ __forceinline__ void skip(int n) {
+        n += s;
+        phase ^= (n / STAGES) & 1;
+        s = n % STAGES;
+    }
+};
+
 template <bool I8, int CG, int PRODUCT, typename Out>
 __global__ void __launch_bounds__(kThreads, 1)
-harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const Params P) {
+harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                 const __grid_constant__ CUtensorMap map_b_small, const Params P) {
     constexpr int BLOCK = I8 ? 128 : 64;                     // contracted elements a stage
+    constexpr int STAGES = CG == 2 ? 6 : 4;                  // one CTA: room for the sums of a split
     constexpr bool A_MN = PRODUCT != FORWARD, B_MN = PRODUCT == GRAD_WEIGHTS;
     constexpr uint32_t COLUMNS = CG == 2 ? 512 : 256;        // two accumulators
     constexpr uint32_t ACC = COLUMNS / 2;
 
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t bars[3 * kMaxStages + 6];
+    __shared__ __align__(8) uint64_t bars[2 * STAGES + 8];
     __shared__ uint32_t s_columns;
     __shared__ int s_dead;
 
@@ -149,23 +171,23 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     const int cluster = blockIdx.x / size, clusters = gridDim.x / size;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     unsigned char *const base_ptr = smem_raw + (base - smem_u32(smem_raw));
-    const uint32_t sums = base + (uint32_t)P.stages * kStage;        // the other ranks' accumulators (split > 1)
-    int *const off = reinterpret_cast<int *>(base_ptr + P.stages * kStage + (P.split > 1 ? P.tile_cols * 512 : 0));
+    const uint32_t sums = base + STAGES * kStage;            // the other ranks' accumulators (split > 1)
+    int *const off = reinterpret_cast<int *>(base_ptr + STAGES * kStage + (CG == 1 && P.split > 1 ? P.tile_cols * 512 : 0));
     int *const first = off + P.n_groups + 1;
 
     const uint32_t bar0 = smem_u32(bars);
-    auto full = [&](int s) { return bar0 + 8u * s; };                            // a stage has arrived
-    auto empty = [&](int s) { return bar0 + 8u * (kMaxStages + s); };            // a stage has been multiplied
-    auto ready = [&](int s) { return bar0 + 8u * (2 * kMaxStages + s); };        // ... is free of other groups' rows in both CTAs (GRAD_WEIGHTS)
-    auto done = [&](int a) { return bar0 + 8u * (3 * kMaxStages + a); };         // an accumulator is complete
-    auto taken = [&](int a) { return bar0 + 8u * (3 * kMaxStages + 2 + a); };    // ... has been read
-    const uint32_t sums_full = bar0 + 8u * (3 * kMaxStages + 4), sums_free = bar0 + 8u * (3 * kMaxStages + 5);
+    auto full = [&](int s) { return bar0 + 8u * s; };                        // a stage has arrived (of a pair: both halves, in the first CTA)
+    auto empty = [&](int s) { return bar0 + 8u * (STAGES + s); };            // a stage has been multiplied
+    auto done = [&](int a) { return bar0 + 8u * (2 * STAGES + a); };         // an accumulator is complete
+    auto taken = [&](int a) { return bar0 + 8u * (2 * STAGES + 2 + a); };    // ... has been read
+    const uint32_t sums_full = bar0 + 8u * (2 * STAGES + 4), sums_free = bar0 + 8u * (2 * STAGES + 5);
+    const uint32_t ragged = bar0 + 8u * (2 * STAGES + 6);                    // this CTA's half of a ragged last block has arrived
+    const uint32_t cleared = bar0 + 8u * (2 * STAGES + 7);                   // ... and the second CTA's is clean
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kMaxStages; ++s) {
+        for (int s = 0; s < STAGES; ++s) {
             mbar_init(full(s), 1);
             mbar_init(empty(s), 1);
-            mbar_init(ready(s), CG);
         }
         for (int a = 0; a < 2; ++a) {
             mbar_init(done(a), 1);
@@ -173,10 +195,13 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         }
         mbar_init(sums_full, 4 * P.split);
         mbar_init(sums_free, 4 * P.split);
+        mbar_init(ragged, 1);
+        mbar_init(cleared, 1);
         mbar_init_fence();
         s_dead = 0;
         prefetch_map(&map_a);
         prefetch_map(&map_b);
+        prefetch_map(&map_b_small);
     }
     if (warp == 2) alloc_columns<CG>(smem_u32(&s_columns), COLUMNS);
     wait_for_previous();
@@ -225,49 +250,55 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     auto from = [&](const Tile &T) { return CG == 2 ? 0 : (int)((int64_t)T.blocks * (int)rank / P.split); };
     auto to = [&](const Tile &T) { return CG == 2 ? T.blocks : (int)((int64_t)T.blocks * ((int)rank + 1) / P.split); };
     auto width = [&](const Tile &T) { return round_up(T.cols, CG == 2 ? 32 : 16); };     // columns of the instruction
+    auto is_ragged = [&](const Tile &T, int b) { return PRODUCT == GRAD_WEIGHTS && b == T.blocks - 1 && T.tail % 16 != 0; };
 
     if (warp == 0 && lane == 0) {
-        int it = 0;
+        Ring<STAGES> ring;
+        uint32_t used = 0;                                   // a bit for each stage that a copy went to
         bool alive = true;
         for (int t = cluster; alive && t < n_tiles; t += clusters) {
             const Tile T = at(t);
             const int half = width(T) / CG;                  // columns of this CTA
-            const int lane0 = T.lane0 + (CG == 2 ? (int)rank * 128 : 0), col0 = (int)rank * (CG == 2 ? half : 0);
-            const int boxes = B_MN ? div_up(half, 64) : div_up(half, P.box_rows);
-            const uint32_t box_bytes = B_MN ? 8192u : (uint32_t)P.box_rows * 128u;
-            const uint32_t bytes = kHalf + (uint32_t)boxes * box_bytes;
-            for (int b = from(T); b < to(T); ++b, ++it) {
-                const int s = it % P.stages;
-                if (!wait(empty(s), ((it / P.stages) & 1) ^ 1, 1)) { alive = false; break; }
+            const int lane0 = T.lane0 + (CG == 2 ? (int)rank * 128 : 0), col0 = CG == 2 ? (int)rank * half : 0;
+            // rows along the columns: one copy of 128 of them, or copies of 32
+            const bool one = B_MN || half > 64;
+            const int boxes = B_MN ? div_up(half, 64) : one ? 1 : div_up(half, 32);
+            const uint32_t bytes = kHalf + (B_MN ? (uint32_t)boxes * 8192u : one ? 16384u : (uint32_t)boxes * 4096u);
+            const int b1 = to(T);
+            for (int b = from(T); b < b1; ++b, ring.next()) {
+                const int s = ring.s;
+                if (!wait(empty(s), ring.phase ^ 1, 1)) { alive = false; break; }
                 const uint32_t a = base + (uint32_t)s * kStage, bb = a + kHalf;
                 uint32_t bar = full(s);
-                if (CG == 2 && PRODUCT != GRAD_WEIGHTS) {    // one barrier, the first CTA's, for both halves
-                    if (rank == 0) mbar_expect_tx(bar, 2 * bytes);
-                    else bar = map_rank(bar, 0);
-                } else mbar_expect_tx(bar, bytes);
+                if (is_ragged(T, b)) mbar_expect_tx(bar = ragged, bytes);
+                else if (CG == 1) mbar_expect_tx(bar, bytes);
+                else if (rank == 0) mbar_expect_tx(bar, 2 * bytes);
+                else bar = map_rank(bar, 0);
+                used |= 1u << s;
                 const int k = b * BLOCK;
                 if (PRODUCT == FORWARD) load_3d<CG>(a, &map_a, k, lane0, T.e, bar);
                 else if (PRODUCT == GRAD_ROWS) {
                     load_3d<CG>(a, &map_a, lane0, k, T.e, bar);
                     load_3d<CG>(a + 8192, &map_a, lane0 + 64, k, T.e, bar);
                 } else {
-                    tma_load_2d(a, &map_a, lane0, T.row0 + k, bar);
-                    tma_load_2d(a + 8192, &map_a, lane0 + 64, T.row0 + k, bar);
+                    load_2d<CG>(a, &map_a, lane0, T.row0 + k, bar);
+                    load_2d<CG>(a + 8192, &map_a, lane0 + 64, T.row0 + k, bar);
                 }
-                for (int i = 0; i < boxes; ++i) {
-                    if (B_MN) tma_load_2d(bb + i * 8192, &map_b, T.col0 + col0 + i * 64, T.row0 + k, bar);
-                    else load_2d<CG>(bb + i * box_bytes, &map_b, k, T.row0 + col0 + i * P.box_rows, bar);
-                }
+                if (B_MN) {
+                    for (int i = 0; i < boxes; ++i) load_2d<CG>(bb + i * 8192, &map_b, T.col0 + col0 + i * 64, T.row0 + k, bar);
+                } else if (one) load_2d<CG>(bb, &map_b, k, T.row0 + col0, bar);
+                else
+                    for (int i = 0; i < boxes; ++i) load_2d<CG>(bb + i * 4096, &map_b_small, k, T.row0 + col0 + i * 32, bar);
             }
         }
-        if (!alive && (rank == 0 || CG == 1 || PRODUCT == GRAD_WEIGHTS))
+        if (!alive) {
             // leave no copy in flight: the last use of every stage, as far as there was one
-            for (int s = 0; s < P.stages && s < it; ++s) {
-                const int use = (it - 1 - s) / P.stages;
-                for (uint32_t i = 0; i < kSpin && !mbar_try(full(s), use & 1); ++i) {}
-            }
+            for (int s = 0; s < STAGES; ++s)
+                for (uint32_t i = 0; (used >> s & 1) && i < kSpin && !mbar_try(full(s), s < ring.s ? ring.phase : ring.phase ^ 1); ++i) {}
+        }
     } else if (warp == 1 && lane == 0 && (CG == 1 || rank == 0)) {
-        int it = 0, n = 0;
+        Ring<STAGES> ring;
+        int n = 0;
         bool alive = true;
         for (int t = cluster; alive && t < n_tiles; t += clusters) {
             const Tile T = at(t);
@@ -278,45 +309,55 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             if (!wait(taken(acc), ((n >> 1) & 1) ^ 1, 2)) break;
             tc_fence_after();
             const uint32_t d = columns + acc * ACC;
-            for (int b = b0; b < b1; ++b, ++it) {
-                const int s = it % P.stages;
-                if (!wait(PRODUCT == GRAD_WEIGHTS ? ready(s) : full(s), (it / P.stages) & 1, 3)) { alive = false; break; }
+            for (int b = b0; b < b1; ++b, ring.next()) {
+                const int s = ring.s;
+                if (!wait(full(s), ring.phase, 3)) { alive = false; break; }
                 tc_fence_after();
                 const uint32_t a = base + (uint32_t)s * kStage;
                 const uint64_t da = A_MN ? operand(a, 8192, 1024) : operand(a, 16, 1024);
                 const uint64_t db = B_MN ? operand(a + kHalf, 8192, 1024) : operand(a + kHalf, 16, 1024);
-                const int steps = PRODUCT == GRAD_WEIGHTS && b == T.blocks - 1 ? div_up(T.tail, 16) : 4;
-                for (int k = 0; k < steps; ++k)
-                    mma_ss<I8, CG>(d, da + (uint64_t)(A_MN ? 128 : 2) * k, db + (uint64_t)(B_MN ? 128 : 2) * k, idesc, b > b0 || k > 0);
+                constexpr uint64_t step_a = A_MN ? 128 : 2, step_b = B_MN ? 128 : 2;
+                if (PRODUCT == GRAD_WEIGHTS && b == T.blocks - 1) {
+                    for (int k = 0; k < div_up(T.tail, 16); ++k) mma_ss<I8, CG>(d, da + step_a * k, db + step_b * k, idesc, b > b0 || k > 0);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) mma_ss<I8, CG>(d, da + step_a * k, db + step_b * k, idesc, b > b0 || k > 0);
+                }
                 commit<CG>(empty(s));
             }
             if (alive && b1 > b0) commit<CG>(done(acc));
             ++n;
         }
     } else if (warp == 2 && PRODUCT == GRAD_WEIGHTS) {
-        int it = 0;
-        bool alive = true;
-        for (int t = cluster; alive && t < n_tiles; t += clusters) {
+        // the other groups' rows of a ragged last block
+        Ring<STAGES> ring;
+        uint32_t phase = 0;
+        for (int t = cluster; t < n_tiles; t += clusters) {
             const Tile T = at(t);
-            const int chunks = 2 + div_up(width(T) / CG, 64);        // of 64 lanes or columns, 64 rows of 128 bytes each
-            for (int b = 0; b < T.blocks; ++b, ++it) {
-                const int s = it % P.stages;
-                if (!wait(full(s), (it / P.stages) & 1, 4)) { alive = false; break; }
-                if (b == T.blocks - 1 && T.tail % 16) {
-                    for (int c = 0; c < chunks; ++c)
-                        for (int r = T.tail; r < round_up(T.tail, 16); ++r)
-                            *reinterpret_cast<uint32_t *>(base_ptr + s * kStage + c * 8192 + r * 128 + lane * 4) = 0;
-                    fence_async_smem();
-                }
+            if (T.blocks == 0) continue;
+            ring.skip(T.blocks - 1);
+            if (is_ragged(T, T.blocks - 1)) {
+                if (!wait(ragged, phase, 4)) break;
+                const int chunks = 2 + div_up(width(T) / CG, 64);    // of 64 lanes or columns, 64 rows of 128 bytes each
+                for (int c = 0; c < chunks; ++c)
+                    for (int r = T.tail; r < round_up(T.tail, 16); ++r)
+                        *reinterpret_cast<uint32_t *>(base_ptr + ring.s * kStage + c * 8192 + r * 128 + lane * 4) = 0;
+                fence_async_smem();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(CG == 2 ? map_rank(ready(s), 0) : ready(s));
+                if (CG == 2 && rank == 1) {
+                    if (lane == 0) mbar_arrive_cluster(map_rank(cleared, 0));
+                } else {
+                    if (CG == 2 && !wait.cluster(cleared, phase, 8)) break;
+                    if (lane == 0) mbar_arrive(full(ring.s));
+                }
+                phase ^= 1;
             }
+            ring.next();
         }
     } else if (warp >= 4) {
         const int q = warp - 4;
         int n = 0;
-        bool alive = true;
-        for (int t = cluster; alive && t < n_tiles; t += clusters) {
+        for (int t = cluster; t < n_tiles; t += clusters) {
             const Tile T = at(t);
             const int l = T.lane0 + (CG == 2 ? (int)rank * 128 : 0) + q * 32 + lane;
             const bool inside = l < P.lanes;
@@ -338,7 +379,7 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             tc_fence_after();
             const uint32_t d = columns + acc * ACC + ((uint32_t)q << 21);
             const int w = width(T);
-            if (P.split == 1) {
+            if (CG == 2 || P.split == 1) {
                 for (int c0 = 0; c0 < w; c0 += 16) {
                     uint32_t v[16];
                     tmem_ld16(d + c0, v);
@@ -355,7 +396,7 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             } else {
                 // columns dealt out to the ranks in runs of `run`; sums[source][column of the run][lane]
                 const int run = div_up(w, P.split);
-                if (!wait(sums_free, (n & 1) ^ 1, 6)) { alive = false; break; }
+                if (!wait(sums_free, (n & 1) ^ 1, 6)) break;
                 for (int c0 = 0; c0 < w; c0 += 16) {
                     uint32_t v[16];
                     if (any) {
@@ -371,8 +412,8 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 }
                 __syncwarp();
                 if (lane < P.split) mbar_arrive_cluster(map_rank(sums_full, lane));
-                if (!wait(sums_full, n & 1, 7)) { alive = false; break; }
-                const uint32_t *const mine = reinterpret_cast<const uint32_t *>(base_ptr + P.stages * kStage) + q * 32 + lane;
+                if (!wait.cluster(sums_full, n & 1, 7)) break;
+                const uint32_t *const mine = reinterpret_cast<const uint32_t *>(base_ptr + STAGES * kStage) + q * 32 + lane;
                 for (int c = 0; c < run; ++c) {
                     const int col = (int)rank * run + c;
                     if (col >= T.cols) break;
@@ -392,7 +433,7 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             }
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive_cluster(CG == 2 ? map_rank(taken(acc), 0) : taken(acc));
+            if (lane == 0) mbar_arrive_at(CG == 2 ? map_rank(taken(acc), 0) : taken(acc));
             ++n;
         }
     }
@@ -424,19 +465,19 @@ bool encode(CUtensorMap *map, bool i8, const void *ptr, int rank, const int64_t 
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-int smem_bytes(const Params &P) {
-    return 1024 + P.stages * kStage + (P.split > 1 ? P.tile_cols * 512 : 0) + 8 * (P.n_groups + 1);
+int smem_bytes(int cg, const Params &P) {
+    return 1024 + (cg == 2 ? 6 : 4) * kStage + (P.split > 1 ? P.tile_cols * 512 : 0) + 8 * (P.n_groups + 1);
 }
 
 template <bool I8, int CG, int PRODUCT, typename Out>
-harp_status_t launch(const CUtensorMap &a, const CUtensorMap &b, const Params &P, int clusters, cudaStream_t s) {
+harp_status_t launch(const CUtensorMap (&maps)[3], const Params &P, int clusters, cudaStream_t s) {
     const auto kernel = harp_gemm_kernel<I8, CG, PRODUCT, Out>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448 - 1024) != cudaSuccess) return HARP_ERR_CUDA;
     const int size = CG == 2 ? 2 : P.split;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(clusters * size));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = (size_t)smem_bytes(P);
+    cfg.dynamicSmemBytes = (size_t)smem_bytes(CG, P);
     cfg.stream = s;
     cudaLaunchAttribute la[2];
     la[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -446,7 +487,7 @@ harp_status_t launch(const CUtensorMap &a, const CUtensorMap &b, const Params &P
     la[1].val.clusterDim.y = la[1].val.clusterDim.z = 1;
     cfg.attrs = la;
     cfg.numAttrs = 2;
-    const cudaError_t err = cudaLaunchKernelEx(&cfg, kernel, a, b, P);
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, kernel, maps[0], maps[1], maps[2], P);
     g_harp_launches.fetch_add(1, std::memory_order_relaxed);
     if (err != cudaSuccess) {
         cudaGetLastError();
@@ -456,8 +497,8 @@ harp_status_t launch(const CUtensorMap &a, const CUtensorMap &b, const Params &P
 }
 
 template <bool I8, int CG, int PRODUCT>
-harp_status_t launch(harp_dtype_t out, const CUtensorMap &a, const CUtensorMap &b, const Params &P, int clusters, cudaStream_t s) {
-    return out == HARP_F32 ? launch<I8, CG, PRODUCT, float>(a, b, P, clusters, s) : launch<I8, CG, PRODUCT, __nv_bfloat16>(a, b, P, clusters, s);
+harp_status_t launch(harp_dtype_t out, const CUtensorMap (&maps)[3], const Params &P, int clusters, cudaStream_t s) {
+    return out == HARP_F32 ? launch<I8, CG, PRODUCT, float>(maps, P, clusters, s) : launch<I8, CG, PRODUCT, __nv_bfloat16>(maps, P, clusters, s);
 }
 
 }  // namespace
@@ -481,7 +522,10 @@ const Device *device() {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)d.sms / 2 * 2);
         cfg.blockDim = dim3(kThreads);
-        cfg.dynamicSmemBytes = 1024 + kMaxStages * kStage + 8 * (kMaxGroups + 1);
+        Params most = {};
+        most.split = 1;
+        most.n_groups = kMaxGroups;
+        cfg.dynamicSmemBytes = (size_t)smem_bytes(2, most);
         cudaLaunchAttribute la;
         la.id = cudaLaunchAttributeClusterDimension;
         la.val.clusterDim.x = 2;
@@ -515,38 +559,34 @@ harp_status_t gemm(const Call &c, const Device &dev, cudaStream_t stream) {
     P.cols = (int32_t)c.d_out;
     P.depth = (int32_t)(c.product == FORWARD ? c.d_in : c.d_out);
     P.tile_cols = 256;
-    P.stages = kMaxStages;
     P.split = 1;
-    int cg = 2;
     int64_t tiles;
-    if (c.product == GRAD_WEIGHTS) {
-        tiles = (int64_t)c.n_groups * ((P.lanes + 255) / 256) * ((P.cols + 255) / 256);
-    } else {
-        tiles = ((int64_t)P.lanes + 255) / 256 * ((c.n_rows + 255) / 256 + c.n_groups - 1);
-        P.box_rows = 32;
-    }
+    if (c.product == GRAD_WEIGHTS) tiles = (int64_t)c.n_groups * ((P.lanes + 255) / 256) * ((P.cols + 255) / 256);
+    else tiles = ((int64_t)P.lanes + 255) / 256 * ((c.n_rows + 255) / 256 + c.n_groups - 1);
     if (tiles > INT32_MAX / 2) return HARP_ERR_TOO_LARGE;
-    const int clusters = (int)std::min<int64_t>(tiles, cg == 2 ? dev.pairs : dev.sms / P.split);
+    const int clusters = (int)std::min<int64_t>(tiles, dev.pairs);
 
-    CUtensorMap a, b;
+    CUtensorMap maps[3];
     const int elems = 128 / es;
     bool ok;
     if (c.product == GRAD_WEIGHTS) {
         const int64_t ea[2] = {c.d_in, c.n_rows}, pa[1] = {c.ld_rows * es}, eb[2] = {c.d_out, c.n_rows}, pb[1] = {c.ld_other * es};
         const int box[2] = {64, 64};
-        ok = encode(&a, false, c.rows, 2, ea, pa, box) && encode(&b, false, c.other, 2, eb, pb, box);
+        ok = encode(&maps[0], false, c.rows, 2, ea, pa, box) && encode(&maps[1], false, c.other, 2, eb, pb, box);
+        maps[2] = maps[1];
     } else {
         const int64_t ea[3] = {c.d_in, c.d_out, c.n_groups}, pa[2] = {c.ld_other * es, c.ld_other * es * c.d_out};
         const int box_a[3] = {elems, c.product == FORWARD ? 128 : 64, 1};
         const int64_t eb[2] = {c.d_rows, c.n_rows}, pb[1] = {c.ld_rows * es};
-        const int box_b[2] = {elems, P.box_rows};
-        ok = encode(&a, c.i8, c.other, 3, ea, pa, box_a) && encode(&b, c.i8, c.rows, 2, eb, pb, box_b);
+        const int box_b[2] = {elems, 128}, box_small[2] = {elems, 32};
+        ok = encode(&maps[0], c.i8, c.other, 3, ea, pa, box_a) && encode(&maps[1], c.i8, c.rows, 2, eb, pb, box_b) &&
+             encode(&maps[2], c.i8, c.rows, 2, eb, pb, box_small);
     }
     if (!ok) return HARP_ERR_UNSUPPORTED;
-    if (c.i8) return launch<true, 2, FORWARD>(c.out_dtype, a, b, P, clusters, stream);
-    if (c.product == FORWARD) return launch<false, 2, FORWARD>(c.out_dtype, a, b, P, clusters, stream);
-    if (c.product == GRAD_ROWS) return launch<false, 2, GRAD_ROWS>(c.out_dtype, a, b, P, clusters, stream);
-    return launch<false, 2, GRAD_WEIGHTS>(c.out_dtype, a, b, P, clusters, stream);
+    if (c.i8) return launch<true, 2, FORWARD>(c.out_dtype, maps, P, clusters, stream);
+    if (c.product == FORWARD) return launch<false, 2, FORWARD>(c.out_dtype, maps, P, clusters, stream);
+    if (c.product == GRAD_ROWS) return launch<false, 2, GRAD_ROWS>(c.out_dtype, maps, P, clusters, stream);
+    return launch<false, 2, GRAD_WEIGHTS>(c.out_dtype, maps, P, clusters, stream);
 }
 
 }  // namespace harp_linear

@@ -22,7 +22,12 @@ __device__ __forceinline__ uint32_t map_rank(uint32_t addr, uint32_t rank) {
     return r;
 }
 __device__ __forceinline__ void mbar_init_fence() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
-// arrival at a barrier of any CTA of the cluster (address from map_rank)
+// Arrivals at a barrier of any CTA of the cluster (address from map_rank): behind tensor-memory reads, which tcgen05.fence orders,
+// and behind stores to shared memory that the other CTA reads (a release across the cluster waits for all of the thread's stores:
+// one at every stage halved the rate of a product).
+__device__ __forceinline__ void mbar_arrive_at(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
