@@ -34,7 +34,7 @@ namespace {
 
 using namespace harp_gemm_ptx;
 
-constexpr int kThreads = 256;                // warps: 0 copies, 1 products, 2 tensor memory and ragged ends, 3 offsets, 4-7 epilogue
+constexpr int kThreads = 384;                // warps: 0 copies, 1 products, 2 tensor memory and ragged ends, 3 offsets, 4-11 epilogue (two a lane quarter)
 constexpr int kHalf = 16384;                 // one operand's part of a stage in one CTA
 constexpr int kStage = 2 * kHalf;
 constexpr uint32_t kSpin = 1u << 22;         // limit of every wait
@@ -51,6 +51,7 @@ struct Params {
     int64_t ld_out, group_out;               // group_out: elements between two groups' outputs (GRAD_WEIGHTS)
     const float *row_scale, *channel_scale;
     int32_t accumulate;
+    int32_t pairs;                           // bf16 results may be stored two lanes at a time
     int32_t *err;
 };
 
@@ -150,6 +151,12 @@ struct Ring {
     }
 };
 
+__device__ __forceinline__ uint32_t pack_bf16(uint32_t lo, uint32_t hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(__uint_as_float(hi)), "f"(__uint_as_float(lo)));
+    return r;
+}
+
 template <bool I8, int CG, int PRODUCT, typename Out>
 __global__ void __launch_bounds__(kThreads, 1)
 harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
@@ -162,6 +169,7 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
 
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t bars[2 * STAGES + 8];
+    __shared__ __align__(16) float s_scale[2][256 + 32];     // rows' scales of two tiles; chunks of 32 columns may run over
     __shared__ uint32_t s_columns;
     __shared__ int s_dead;
 
@@ -191,10 +199,10 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         }
         for (int a = 0; a < 2; ++a) {
             mbar_init(done(a), 1);
-            mbar_init(taken(a), 4 * CG);
+            mbar_init(taken(a), 8 * CG);
         }
-        mbar_init(sums_full, 4 * P.split);
-        mbar_init(sums_free, 4 * P.split);
+        mbar_init(sums_full, 8 * P.split);
+        mbar_init(sums_free, 8 * P.split);
         mbar_init(ragged, 1);
         mbar_init(cleared, 1);
         mbar_init_fence();
@@ -355,7 +363,7 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             ring.next();
         }
     } else if (warp >= 4) {
-        const int q = warp - 4;
+        const int q = warp & 3, part = (warp - 4) >> 2;      // lanes 32 q .. 32 q + 31; chunks of 32 columns alternate between the two warps
         int n = 0;
         for (int t = cluster; t < n_tiles; t += clusters) {
             const Tile T = at(t);
@@ -364,40 +372,65 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             Out *const out = static_cast<Out *>(P.out) +
                 (PRODUCT == GRAD_WEIGHTS ? T.e * P.group_out + (int64_t)T.col0 * P.ld_out : (int64_t)T.row0 * P.ld_out) + l;
             const float by_lane = I8 && inside ? P.channel_scale[(int64_t)T.e * P.lanes + l] : 1.0f;
-            auto put = [&](int c, float v) {
-                if (PRODUCT == GRAD_WEIGHTS && P.accumulate) v += load(out + (int64_t)c * P.ld_out);
-                store(out + (int64_t)c * P.ld_out, v);
-            };
             if (T.blocks == 0) {                             // a group without rows
                 if (inside && !P.accumulate)
-                    for (int c = 0; c < T.cols; ++c) store(out + (int64_t)c * P.ld_out, 0.0f);
+                    for (int c = part; c < T.cols; c += 2) store(out + (int64_t)c * P.ld_out, 0.0f);
                 continue;
             }
             const int acc = n & 1;
             const bool any = to(T) > from(T);
+            if (I8 && (CG == 2 || P.split == 1)) {           // the rows' scales, for all the columns of the tile
+                const int c = threadIdx.x - 128;
+                if (c < T.cols) s_scale[acc][c] = P.row_scale[T.row0 + c];
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+            }
             if (any && !wait(done(acc), (n >> 1) & 1, 5)) break;
             tc_fence_after();
             const uint32_t d = columns + acc * ACC + ((uint32_t)q << 21);
             const int w = width(T);
             if (CG == 2 || P.split == 1) {
-                for (int c0 = 0; c0 < w; c0 += 16) {
-                    uint32_t v[16];
-                    tmem_ld16(d + c0, v);
+                const bool pairs = sizeof(Out) == 2 && P.pairs;
+                for (int c0 = part * 32; c0 < w; c0 += 64) {
+                    uint32_t v[32];
+                    tmem_ld32(d + c0, v);
                     tmem_wait_ld();
-                    if (inside) {
+                    if (I8) {
+                        const float4 *const by_row = reinterpret_cast<const float4 *>(&s_scale[acc][c0]);
 #pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            if (c0 + j < T.cols) {
-                                const float x = I8 ? (float)(int32_t)v[j] * by_lane * P.row_scale[T.row0 + c0 + j] : __uint_as_float(v[j]);
-                                put(c0 + j, x);
-                            }
+                        for (int j = 0; j < 32; j += 4) {
+                            const float4 r = by_row[j / 4];
+                            v[j] = __float_as_uint((float)(int32_t)v[j] * by_lane * r.x);
+                            v[j + 1] = __float_as_uint((float)(int32_t)v[j + 1] * by_lane * r.y);
+                            v[j + 2] = __float_as_uint((float)(int32_t)v[j + 2] * by_lane * r.z);
+                            v[j + 3] = __float_as_uint((float)(int32_t)v[j + 3] * by_lane * r.w);
+                        }
+                    }
+                    if (pairs) {
+                        // neighbouring lanes trade halves of two columns: either then stores both lanes' elements of one
+                        const int odd = lane & 1;
+                        Out *p = out - odd + (int64_t)(c0 + odd) * P.ld_out;
+                        const int left = inside ? T.cols - c0 - odd : 0;
+#pragma unroll
+                        for (int j = 0; j < 32; j += 2) {
+                            const uint32_t got = __shfl_xor_sync(~0u, odd ? v[j] : v[j + 1], 1);
+                            const uint32_t both = pack_bf16(odd ? got : v[j], odd ? v[j + 1] : got);
+                            if (j < left) *reinterpret_cast<uint32_t *>(p) = both;
+                            p += 2 * P.ld_out;
+                        }
+                    } else if (inside) {
+                        Out *p = out + (int64_t)c0 * P.ld_out;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) {
+                            if (c0 + j < T.cols) store(p, __uint_as_float(v[j]) + (PRODUCT == GRAD_WEIGHTS && P.accumulate ? load(p) : 0.0f));
+                            p += P.ld_out;
+                        }
                     }
                 }
             } else {
                 // columns dealt out to the ranks in runs of `run`; sums[source][column of the run][lane]
                 const int run = div_up(w, P.split);
                 if (!wait(sums_free, (n & 1) ^ 1, 6)) break;
-                for (int c0 = 0; c0 < w; c0 += 16) {
+                for (int c0 = part * 16; c0 < w; c0 += 32) {
                     uint32_t v[16];
                     if (any) {
                         tmem_ld16(d + c0, v);
@@ -414,7 +447,7 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 if (lane < P.split) mbar_arrive_cluster(map_rank(sums_full, lane));
                 if (!wait.cluster(sums_full, n & 1, 7)) break;
                 const uint32_t *const mine = reinterpret_cast<const uint32_t *>(base_ptr + STAGES * kStage) + q * 32 + lane;
-                for (int c = 0; c < run; ++c) {
+                for (int c = part; c < run; c += 2) {
                     const int col = (int)rank * run + c;
                     if (col >= T.cols) break;
                     float x;
@@ -426,7 +459,7 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                         x = 0.0f;
                         for (int r = 0; r < P.split; ++r) x += __uint_as_float(mine[(r * run + c) * 128]);
                     }
-                    if (inside) put(col, x);
+                    if (inside) store(out + (int64_t)col * P.ld_out, x);
                 }
                 __syncwarp();
                 if (lane < P.split) mbar_arrive_cluster(map_rank(sums_free, lane));
@@ -472,7 +505,7 @@ int smem_bytes(int cg, const Params &P) {
 template <bool I8, int CG, int PRODUCT, typename Out>
 harp_status_t launch(const CUtensorMap (&maps)[3], const Params &P, int clusters, cudaStream_t s) {
     const auto kernel = harp_gemm_kernel<I8, CG, PRODUCT, Out>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448 - 1024) != cudaSuccess) return HARP_ERR_CUDA;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448 - 4096) != cudaSuccess) return HARP_ERR_CUDA;
     const int size = CG == 2 ? 2 : P.split;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(clusters * size));
@@ -532,7 +565,7 @@ const Device *device() {
         la.val.clusterDim.y = la.val.clusterDim.z = 1;
         cfg.attrs = &la;
         cfg.numAttrs = 1;
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448 - 1024) != cudaSuccess ||
+        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448 - 4096) != cudaSuccess ||
             cudaOccupancyMaxActiveClusters(&d.pairs, kernel, &cfg) != cudaSuccess || d.pairs < 1) {
             cudaGetLastError();
             return;
@@ -558,6 +591,7 @@ harp_status_t gemm(const Call &c, const Device &dev, cudaStream_t stream) {
     P.lanes = (int32_t)(c.product == FORWARD ? c.d_out : c.d_in);
     P.cols = (int32_t)c.d_out;
     P.depth = (int32_t)(c.product == FORWARD ? c.d_in : c.d_out);
+    P.pairs = reinterpret_cast<uintptr_t>(c.out) % 4 == 0 && c.ld_out % 2 == 0 && P.lanes % 2 == 0 && !c.accumulate;
     P.tile_cols = 256;
     P.split = 1;
     int64_t tiles;
