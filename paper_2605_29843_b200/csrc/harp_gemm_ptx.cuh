@@ -63,6 +63,14 @@ __device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap *map, in
 }
 
 template <int CG>
+__device__ __forceinline__ void load_4d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, uint32_t bar) {
+    if (CG == 1) tma_load_4d(dst, map, x, y, z, w, bar);
+    else
+        asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar) : "memory");
+}
+
+template <int CG>
 __device__ __forceinline__ void alloc_columns(uint32_t dst_smem, uint32_t ncols) {
     if (CG == 1) tmem_alloc(dst_smem, ncols);
     else {
