@@ -21,6 +21,7 @@
 // along the columns; in GRAD_WEIGHTS a warp overwrites them with zeros before the products, in both
 // operands, because the other group's values may be infinite.
 #include <algorithm>
+#include <cmath>
 #include <mutex>
 
 #include <cuda.h>
@@ -35,8 +36,12 @@ namespace {
 using namespace harp_gemm_ptx;
 
 constexpr int kThreads = 384;                // warps: 0 copies, 1 products, 2 tensor memory and ragged ends, 3 offsets, 4-11 epilogue (two a lane quarter)
-constexpr int kHalf = 16384;                 // one operand's part of a stage in one CTA
-constexpr int kStage = 2 * kHalf;
+constexpr int kHalf = 16384;                 // the lane operand's part of a stage in one CTA
+constexpr int kPrefetch = 8;                 // blocks of a weight that one CTA asks for before its turn
+constexpr int kSumCols = 32;                 // columns whose sums a split adds up at a time
+// COLS: most columns of a tile (256 for a pair of CTAs, 32 or 64 for one)
+__host__ __device__ constexpr int stage_bytes(int cols) { return kHalf + (cols == 256 ? 128 : cols) * 128; }
+__host__ __device__ constexpr int stages(int cols) { return cols == 256 ? 6 : cols == 64 ? 3 : 4; }      // one CTA leaves room for another one
 constexpr uint32_t kSpin = 1u << 22;         // limit of every wait
 
 __device__ int32_t g_gemm_err;
@@ -152,25 +157,26 @@ struct Ring {
     }
 };
 
+__device__ __forceinline__ uint32_t add(uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }
 __device__ __forceinline__ uint32_t pack_bf16(uint32_t lo, uint32_t hi) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(__uint_as_float(hi)), "f"(__uint_as_float(lo)));
     return r;
 }
 
-template <bool I8, int CG, int PRODUCT, typename Out>
-__global__ void __launch_bounds__(kThreads, 1)
+template <bool I8, int COLS, int PRODUCT, typename Out>
+__global__ void __launch_bounds__(kThreads, COLS == 256 ? 1 : 2)
 harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                  const __grid_constant__ CUtensorMap map_b_small, const Params P) {
     constexpr int BLOCK = I8 ? 128 : 64;                     // contracted elements a stage
-    constexpr int STAGES = CG == 2 ? 6 : 4;                  // one CTA: room for the sums of a split
+    constexpr int CG = COLS == 256 ? 2 : 1;                  // CTAs a tile
+    constexpr int STAGES = stages(COLS), kStage = stage_bytes(COLS);
     constexpr bool A_MN = PRODUCT != FORWARD, B_MN = PRODUCT == GRAD_WEIGHTS;
-    constexpr uint32_t COLUMNS = CG == 2 ? 512 : 256;        // two accumulators
-    constexpr uint32_t ACC = COLUMNS / 2;
+    constexpr uint32_t COLUMNS = 2 * COLS, ACC = COLS;       // two accumulators
 
     extern __shared__ unsigned char smem_raw[];
-    __shared__ __align__(8) uint64_t bars[2 * STAGES + 8];
-    __shared__ __align__(16) float s_scale[2][256 + 32];     // rows' scales of two tiles; chunks of 32 columns may run over
+    __shared__ __align__(8) uint64_t bars[4 * STAGES + 6];
+    __shared__ __align__(16) float s_scale[8][32];           // rows' scales of a chunk of columns, by epilogue warp
     __shared__ uint32_t s_columns;
     __shared__ int s_dead;
 
@@ -181,7 +187,7 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     unsigned char *const base_ptr = smem_raw + (base - smem_u32(smem_raw));
     const uint32_t sums = base + STAGES * kStage;            // the other ranks' accumulators (split > 1)
-    int *const off = reinterpret_cast<int *>(base_ptr + STAGES * kStage + (CG == 1 && P.split > 1 ? P.tile_cols * 512 : 0));
+    int *const off = reinterpret_cast<int *>(base_ptr + STAGES * kStage + (CG == 1 && P.split > 1 ? kSumCols * 512 : 0));
     int *const first = off + P.n_groups + 1;
 
     const uint32_t bar0 = smem_u32(bars);
@@ -190,33 +196,32 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     auto done = [&](int a) { return bar0 + 8u * (2 * STAGES + a); };         // an accumulator is complete
     auto taken = [&](int a) { return bar0 + 8u * (2 * STAGES + 2 + a); };    // ... has been read
     const uint32_t sums_full = bar0 + 8u * (2 * STAGES + 4), sums_free = bar0 + 8u * (2 * STAGES + 5);
-    const uint32_t ragged = bar0 + 8u * (2 * STAGES + 6);                    // this CTA's half of a ragged last block has arrived
-    const uint32_t cleared = bar0 + 8u * (2 * STAGES + 7);                   // ... and the second CTA's is clean
+    // one of either a stage: with few blocks a tile the copies are several ragged blocks ahead
+    auto ragged = [&](int s) { return bar0 + 8u * (2 * STAGES + 6 + s); };   // this CTA's half of a ragged last block has arrived
+    auto cleared = [&](int s) { return bar0 + 8u * (3 * STAGES + 6 + s); };  // ... and the second CTA's is clean
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(full(s), 1);
             mbar_init(empty(s), 1);
+            mbar_init(ragged(s), 1);
+            mbar_init(cleared(s), 1);
         }
         for (int a = 0; a < 2; ++a) {
             mbar_init(done(a), 1);
             mbar_init(taken(a), 8 * CG);
         }
-        mbar_init(sums_full, 8 * P.split);
+        mbar_init(sums_full, 1);
         mbar_init(sums_free, 8 * P.split);
-        mbar_init(ragged, 1);
-        mbar_init(cleared, 1);
         mbar_init_fence();
         s_dead = 0;
         prefetch_map(&map_a);
         prefetch_map(&map_b);
         prefetch_map(&map_b_small);
     }
-    if (warp == 2) alloc_columns<CG>(smem_u32(&s_columns), COLUMNS);
-    wait_for_previous();
-    launch_dependents();
-    if (warp == 3) {
-        // offsets made to rise and to stay within the batch, and the number of tiles before each group
+    if (warp == 2) alloc_columns<CG, COLUMNS>(smem_u32(&s_columns));
+    // offsets made to rise and to stay within the batch, and the number of tiles before each group
+    auto lay_out = [&] {
         int before = 0, tiles = 0;
         for (int e0 = 0; e0 <= P.n_groups; e0 += 32) {
             const int e = e0 + lane;
@@ -245,11 +250,24 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             before = __shfl_sync(~0u, o, 31);
             tiles += __shfl_sync(~0u, n, 31);
         }
-    }
+    };
+    if (warp == 3 && P.offsets == nullptr) lay_out();
     tc_fence_before();
     if (size > 1) cluster_sync();
     else __syncthreads();
     tc_fence_after();
+    if (CG == 1 && PRODUCT == FORWARD && P.offsets == nullptr && warp == 0 && lane == 0 && cluster < first[1]) {
+        // The first blocks of the weight, into L2: whatever the kernels before this one still write, L2 is where it meets.
+        const Tile T = tile_at<CG, PRODUCT, BLOCK>(cluster, P, off, first);
+        const int b0 = (int)((int64_t)T.blocks * (int)rank / P.split), b1 = (int)((int64_t)T.blocks * ((int)rank + 1) / P.split);
+        for (int b = b0; b < min(b1, b0 + kPrefetch); ++b) prefetch_3d(&map_a, b * BLOCK, T.lane0, 0);
+    }
+    wait_for_previous();
+    launch_dependents();
+    if (P.offsets) {
+        if (warp == 3) lay_out();
+        __syncthreads();
+    }
 
     const uint32_t columns = s_columns;
     const Waiter wait{&s_dead, P.err};
@@ -270,7 +288,7 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             const int half = width(T) / CG;                  // columns of this CTA
             const int lane0 = T.lane0 + (CG == 2 ? (int)rank * 128 : 0), col0 = CG == 2 ? (int)rank * half : 0;
             // rows along the columns: one copy of 128 of them, or copies of 32
-            const bool one = B_MN || half > 64;
+            const bool one = B_MN || (CG == 2 && half > 32);
             const int boxes = B_MN ? div_up(half, 64) : one ? 1 : div_up(half, 32);
             const uint32_t bytes = kHalf + (B_MN ? (uint32_t)boxes * 8192u : one ? 16384u : (uint32_t)boxes * 4096u);
             const int b1 = to(T);
@@ -279,7 +297,7 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 if (!wait(empty(s), ring.phase ^ 1, 1)) { alive = false; break; }
                 const uint32_t a = base + (uint32_t)s * kStage, bb = a + kHalf;
                 uint32_t bar = full(s);
-                if (is_ragged(T, b)) mbar_expect_tx(bar = ragged, bytes);
+                if (is_ragged(T, b)) mbar_expect_tx(bar = ragged(s), bytes);
                 else if (CG == 1) mbar_expect_tx(bar, bytes);
                 else if (rank == 0) mbar_expect_tx(bar, 2 * bytes);
                 else bar = map_rank(bar, 0);
@@ -303,8 +321,8 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     for (int i = 0; i < boxes; ++i) load_2d<CG>(bb + i * 4096, &map_b_small, k, T.row0 + col0 + i * 32, bar);
             }
         }
-        if (!alive) {
-            // leave no copy in flight: the last use of every stage, as far as there was one
+        if (!alive && (CG == 1 || rank == 0)) {
+            // leave no copy in flight, of either CTA: the last use of every stage, as far as there was one
             for (int s = 0; s < STAGES; ++s)
                 for (uint32_t i = 0; (used >> s & 1) && i < kSpin && !mbar_try(full(s), s < ring.s ? ring.phase : ring.phase ^ 1); ++i) {}
         }
@@ -343,13 +361,15 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     } else if (warp == 2 && PRODUCT == GRAD_WEIGHTS) {
         // the other groups' rows of a ragged last block
         Ring<STAGES> ring;
-        uint32_t phase = 0;
+        uint32_t phases = 0;                                 // a bit a stage: its next ragged block's phase
         for (int t = cluster; t < n_tiles; t += clusters) {
             const Tile T = at(t);
             if (T.blocks == 0) continue;
             ring.skip(T.blocks - 1);
             if (is_ragged(T, T.blocks - 1)) {
-                if (!wait(ragged, phase, 4)) break;
+                const uint32_t phase = phases >> ring.s & 1;
+                phases ^= 1u << ring.s;
+                if (!wait(ragged(ring.s), phase, 4)) break;
                 const int chunks = 2 + div_up(width(T) / CG, 64);    // of 64 lanes or columns, 64 rows of 128 bytes each
                 for (int c = 0; c < chunks; ++c)
                     for (int r = T.tail; r < round_up(T.tail, 16); ++r)
@@ -357,18 +377,19 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 fence_async_smem();
                 __syncwarp();
                 if (CG == 2 && rank == 1) {
-                    if (lane == 0) mbar_arrive_cluster(map_rank(cleared, 0));
+                    if (lane == 0) mbar_arrive_cluster(map_rank(cleared(ring.s), 0));
                 } else {
-                    if (CG == 2 && !wait.cluster(cleared, phase, 8)) break;
+                    if (CG == 2 && !wait.cluster(cleared(ring.s), phase, 8)) break;
                     if (lane == 0) mbar_arrive(full(ring.s));
                 }
-                phase ^= 1;
             }
             ring.next();
         }
     } else if (warp >= 4) {
         const int q = warp & 3, part = (warp - 4) >> 2;      // lanes 32 q .. 32 q + 31; chunks of 32 columns alternate between the two warps
         int n = 0;
+        uint32_t sums_phase = 0;
+        bool alive = true;
         for (int t = cluster; t < n_tiles; t += clusters) {
             const Tile T = at(t);
             const int l = T.lane0 + (CG == 2 ? (int)rank * 128 : 0) + q * 32 + lane;
@@ -383,10 +404,13 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             }
             const int acc = n & 1;
             const bool any = to(T) > from(T);
-            if (I8 && (CG == 2 || P.split == 1)) {           // the rows' scales, for all the columns of the tile
-                const int c = threadIdx.x - 128;
-                if (c < T.cols) s_scale[acc][c] = P.row_scale[T.row0 + c];
-                asm volatile("bar.sync 1, 256;" ::: "memory");
+            float by_row[COLS / 64 ? COLS / 64 : 1];         // 8 bits: the rows' scales of this warp's chunks, a lane's column of each
+            if (I8 && (CG == 2 || P.split == 1)) {
+#pragma unroll
+                for (int i = 0; i < (int)(sizeof by_row / sizeof by_row[0]); ++i) {
+                    const int c = (2 * i + part) * 32 + lane;
+                    by_row[i] = c < T.cols ? P.row_scale[T.row0 + c] : 0.0f;
+                }
             }
             if (any && !wait(done(acc), (n >> 1) & 1, 5)) break;
             tc_fence_after();
@@ -394,15 +418,23 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             const int w = width(T);
             if (CG == 2 || P.split == 1) {
                 const bool pairs = sizeof(Out) == 2 && P.pairs;
-                for (int c0 = part * 32; c0 < w; c0 += 64) {
+#pragma unroll
+                for (int i = 0; i < (int)(sizeof by_row / sizeof by_row[0]); ++i) {
+                    const int c0 = (2 * i + part) * 32;
+                    if (c0 >= w) break;
                     uint32_t v[32];
                     tmem_ld32(d + c0, v);
+                    if (I8) {
+                        __syncwarp();
+                        s_scale[warp - 4][lane] = by_row[i];
+                        __syncwarp();
+                    }
                     tmem_wait_ld();
                     if (I8) {
-                        const float4 *const by_row = reinterpret_cast<const float4 *>(&s_scale[acc][c0]);
+                        const float4 *const scale = reinterpret_cast<const float4 *>(s_scale[warp - 4]);
 #pragma unroll
                         for (int j = 0; j < 32; j += 4) {
-                            const float4 r = by_row[j / 4];
+                            const float4 r = scale[j / 4];
                             v[j] = __float_as_uint((float)(int32_t)v[j] * by_lane * r.x);
                             v[j + 1] = __float_as_uint((float)(int32_t)v[j + 1] * by_lane * r.y);
                             v[j + 2] = __float_as_uint((float)(int32_t)v[j + 2] * by_lane * r.z);
@@ -431,42 +463,57 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     }
                 }
             } else {
-                // columns dealt out to the ranks in runs of `run`; sums[source][column of the run][lane]
-                const int run = div_up(w, P.split);
-                if (!wait(sums_free, (n & 1) ^ 1, 6)) break;
-                for (int c0 = part * 16; c0 < w; c0 += 32) {
-                    uint32_t v[16];
-                    if (any) {
-                        tmem_ld16(d + c0, v);
-                        tmem_wait_ld();
-                    }
+                // 32 columns at a time, dealt out to the ranks in runs of 4 to 16; sums[source][four columns of the run][lane][4]
+                for (int h = 0; h < w; h += kSumCols, sums_phase ^= 1) {
+                    const int run = min(w - h, kSumCols) / P.split, shift = 31 - __clz(run);       // powers of two, as 16, 32 and the split are
+                    if (threadIdx.x == 128) mbar_expect_tx(sums_full, (uint32_t)(P.split * run * 512));
+                    if (!wait(sums_free, sums_phase ^ 1, 6)) { alive = false; break; }
+                    const int c0 = h + part * 16;
+                    if (c0 < w) {
+                        uint32_t v[16];
+                        if (any) {
+                            tmem_ld16(d + c0, v);
+                            tmem_wait_ld();
+                        }
 #pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        if (c0 + j < T.cols) {
-                            const int to_rank = (c0 + j) / run, c = (c0 + j) - to_rank * run;
-                            st_cluster(map_rank(sums + (uint32_t)(((int)rank * run + c) * 128 + q * 32 + lane) * 4, to_rank), any ? v[j] : 0u);
+                        for (int j = 0; j < 16; j += 4) {
+                            const int to_rank = (part * 16 + j) >> shift, c = (part * 16 + j) & (run - 1);
+                            const uint32_t place = sums + (uint32_t)(((((int)rank * run + c) >> 2) * 128 + q * 32 + lane) * 16);
+                            send16(map_rank(place, to_rank), any ? v[j] : 0u, any ? v[j + 1] : 0u, any ? v[j + 2] : 0u, any ? v[j + 3] : 0u,
+                                   map_rank(sums_full, to_rank));
+                        }
+                    }
+                    if (!wait.cluster(sums_full, sums_phase, 7)) { alive = false; break; }
+                    const uint4 *const mine = reinterpret_cast<const uint4 *>(base_ptr + STAGES * kStage) + q * 32 + lane;
+                    float x[2][4];                           // this warp's columns: every other four of at most sixteen
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int c = (2 * i + part) * 4;
+                        if (c < run) {
+                            uint4 sum = make_uint4(0, 0, 0, 0);
+                            for (int r = 0; r < P.split; ++r) {
+                                const uint4 s = mine[((r * run + c) >> 2) * 128];
+                                if (I8) sum.x += s.x, sum.y += s.y, sum.z += s.z, sum.w += s.w;
+                                else sum.x = add(sum.x, s.x), sum.y = add(sum.y, s.y), sum.z = add(sum.z, s.z), sum.w = add(sum.w, s.w);
+                            }
+                            x[i][0] = I8 ? (float)(int32_t)sum.x : __uint_as_float(sum.x);
+                            x[i][1] = I8 ? (float)(int32_t)sum.y : __uint_as_float(sum.y);
+                            x[i][2] = I8 ? (float)(int32_t)sum.z : __uint_as_float(sum.z);
+                            x[i][3] = I8 ? (float)(int32_t)sum.w : __uint_as_float(sum.w);
+                        }
+                    }
+                    __syncwarp();
+                    if (lane < P.split) mbar_arrive_at(map_rank(sums_free, lane));
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int c = (2 * i + part) * 4 + j, col = h + (int)rank * run + c;
+                            if (inside && c < run && col < T.cols)
+                                store(out + (int64_t)col * P.ld_out, I8 ? x[i][j] * by_lane * P.row_scale[T.row0 + col] : x[i][j]);
                         }
                 }
-                __syncwarp();
-                if (lane < P.split) mbar_arrive_cluster(map_rank(sums_full, lane));
-                if (!wait.cluster(sums_full, n & 1, 7)) break;
-                const uint32_t *const mine = reinterpret_cast<const uint32_t *>(base_ptr + STAGES * kStage) + q * 32 + lane;
-                for (int c = part; c < run; c += 2) {
-                    const int col = (int)rank * run + c;
-                    if (col >= T.cols) break;
-                    float x;
-                    if (I8) {
-                        int32_t sum = 0;
-                        for (int r = 0; r < P.split; ++r) sum += (int32_t)mine[(r * run + c) * 128];
-                        x = (float)sum * by_lane * P.row_scale[T.row0 + col];
-                    } else {
-                        x = 0.0f;
-                        for (int r = 0; r < P.split; ++r) x += __uint_as_float(mine[(r * run + c) * 128]);
-                    }
-                    if (inside) store(out + (int64_t)col * P.ld_out, x);
-                }
-                __syncwarp();
-                if (lane < P.split) mbar_arrive_cluster(map_rank(sums_free, lane));
+                if (!alive) break;
             }
             tc_fence_before();
             __syncwarp();
@@ -480,7 +527,7 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     else __syncthreads();
     if (warp == 2) {
         tc_fence_after();
-        free_columns<CG>(columns, COLUMNS);
+        free_columns<CG, COLUMNS>(columns);
     }
 }
 
@@ -502,19 +549,19 @@ bool encode(CUtensorMap *map, bool i8, const void *ptr, int rank, const int64_t 
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-int smem_bytes(int cg, const Params &P) {
-    return 1024 + (cg == 2 ? 6 : 4) * kStage + (P.split > 1 ? P.tile_cols * 512 : 0) + 8 * (P.n_groups + 1);
+int smem_bytes(int cols, int split, int n_groups) {
+    return 1024 + stages(cols) * stage_bytes(cols) + (split > 1 ? kSumCols * 512 : 0) + 8 * (n_groups + 1);
 }
 
-template <bool I8, int CG, int PRODUCT, typename Out>
+template <bool I8, int COLS, int PRODUCT, typename Out>
 harp_status_t launch(const CUtensorMap (&maps)[3], const Params &P, int clusters, cudaStream_t s) {
-    const auto kernel = harp_gemm_kernel<I8, CG, PRODUCT, Out>;
+    const auto kernel = harp_gemm_kernel<I8, COLS, PRODUCT, Out>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448 - 4096) != cudaSuccess) return HARP_ERR_CUDA;
-    const int size = CG == 2 ? 2 : P.split;
+    const int size = COLS == 256 ? 2 : P.split;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(clusters * size));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = (size_t)smem_bytes(CG, P);
+    cfg.dynamicSmemBytes = (size_t)smem_bytes(COLS, P.split, P.n_groups);
     cfg.stream = s;
     cudaLaunchAttribute la[2];
     la[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -533,9 +580,59 @@ harp_status_t launch(const CUtensorMap (&maps)[3], const Params &P, int clusters
     return HARP_OK;
 }
 
-template <bool I8, int CG, int PRODUCT>
+template <bool I8, int COLS, int PRODUCT>
 harp_status_t launch(harp_dtype_t out, const CUtensorMap (&maps)[3], const Params &P, int clusters, cudaStream_t s) {
-    return out == HARP_F32 ? launch<I8, CG, PRODUCT, float>(maps, P, clusters, s) : launch<I8, CG, PRODUCT, __nv_bfloat16>(maps, P, clusters, s);
+    return out == HARP_F32 ? launch<I8, COLS, PRODUCT, float>(maps, P, clusters, s) : launch<I8, COLS, PRODUCT, __nv_bfloat16>(maps, P, clusters, s);
+}
+
+// How a call is cut: by pairs of CTAs on 256 lanes x 256 columns, or by single ones on 128 x 32 or 128 x 64 in clusters of `split`.
+struct Shape {
+    int cols, split, slots;              // slots: clusters (pairs) that run at once
+    int64_t tiles;                       // at most
+};
+
+// The cut with the least estimated time: the weight's bytes at the rate of memory, stretched by a last round of tiles that leaves SMs
+// idle, or rounds of tiles times their blocks of 128 contracted bytes.  Constants from 8-bit products of 1 to 2048 rows, widths 2048 to 28672,
+// and 8 to 64 groups of 1 to 128 rows, each cut every way (us a call):
+//                                pairs   32 cols, split 1, 2, 4   64 cols, split 1, 2, 4
+//    16 rows, 14336 -> 4096       40.3    35.4   22.1   17.3       41.0   25.9   19.0
+//    64 rows, 4096 -> 14336       15.5    16.8   19.4   20.5       18.9   19.1   18.4
+//    64 rows, 8192 -> 28672       52.1    53.3   56.1   54.3       43.5   46.9   50.7
+//   128 rows, 14336 -> 4096       36.1    36.3   25.0   26.3       43.8   28.9   21.7
+//   256 rows, 14336 -> 4096       37.1    38.6   44.1   47.0       44.3   30.9   32.5
+//   256 rows, 4096 -> 14336       17.4    45.4   56.1   84.1       30.1   35.8   44.1
+//   8 x 16 rows, 4096 -> 14336   173.9   159.2  147.7  148.4      162.8  154.4  152.6     (bf16)
+//   64 x 64 rows, 2048 -> 2048    55.1    61.7   72.6  116.7       54.7   62.6  100.8
+Shape choose(const Call &c, const Device &dev) {
+    const int64_t lanes = c.product == FORWARD ? c.d_out : c.d_in, pair_tiles = (lanes + 255) / 256, tiles = (lanes + 127) / 128;
+    if (c.product == GRAD_WEIGHTS) return {256, 1, dev.pairs, c.n_groups * pair_tiles * ((c.d_out + 255) / 256)};
+    const Shape pairs = {256, 1, dev.pairs, pair_tiles * ((c.n_rows + 255) / 256 + c.n_groups - 1)};
+    if (c.product == GRAD_ROWS) return pairs;
+    // rows of a group, and half as many again where there are several: they are not even
+    const int64_t met = std::min<int64_t>(c.n_groups, c.n_rows), even = (c.n_rows + met - 1) / met, rows = met > 1 ? even + even / 2 : even;
+    const double blocks = (double)((c.d_in * (c.i8 ? 1 : 2) + 127) / 128), memory = (double)(met * tiles) * blocks * 16384 / 6.3e6;     // us
+    auto cols_of = [&](int most) { return (double)((rows + most - 1) / most); };
+    Shape best = pairs;
+    double least;
+    {
+        const double n = (double)(met * pair_tiles) * cols_of(256), rounds = std::ceil(n / dev.pairs);
+        const double width = std::min<double>(256, (double)rows / cols_of(256));
+        const double stretch = rounds > 1 ? rounds * dev.pairs / n : 1;
+        least = std::max(memory * stretch, rounds * (blocks * (0.29 + 0.00037 * width) + 0.5)) + 4.5;
+    }
+    for (int cols = 32; cols <= 64; cols *= 2)
+        for (int i = 0; i < 3; ++i) {
+            const double n = (double)(met * tiles) * cols_of(cols), rounds = std::ceil(n / dev.clusters[i]);
+            const double stretch = rounds > 1 ? 0.75 + 0.25 * rounds * dev.clusters[i] / n : 1;
+            const double join = i ? (cols == 32 ? 2.5 : 4) : 0.5;        // adding up a tile's sums
+            const double block = n * (1 << i) > dev.sms ? (cols == 32 ? 0.33 : 0.42) : (cols == 32 ? 0.285 : 0.36);
+            const double t = std::max(memory * stretch, rounds * (blocks / (1 << i) * block + join)) + 3.5;
+            if (dev.clusters[i] > 0 && t < least) {
+                least = t;
+                best = {cols, 1 << i, dev.clusters[i], tiles * ((c.n_rows + cols - 1) / cols + c.n_groups - 1)};
+            }
+        }
+    return best;
 }
 
 }  // namespace
@@ -555,25 +652,29 @@ const Device *device() {
             return;
         }
         d.err = static_cast<int32_t *>(err);
-        const auto kernel = harp_gemm_kernel<false, 2, FORWARD, __nv_bfloat16>;
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)d.sms / 2 * 2);
-        cfg.blockDim = dim3(kThreads);
-        Params most = {};
-        most.split = 1;
-        most.n_groups = kMaxGroups;
-        cfg.dynamicSmemBytes = (size_t)smem_bytes(2, most);
-        cudaLaunchAttribute la;
-        la.id = cudaLaunchAttributeClusterDimension;
-        la.val.clusterDim.x = 2;
-        la.val.clusterDim.y = la.val.clusterDim.z = 1;
-        cfg.attrs = &la;
-        cfg.numAttrs = 1;
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448 - 4096) != cudaSuccess ||
-            cudaOccupancyMaxActiveClusters(&d.pairs, kernel, &cfg) != cudaSuccess || d.pairs < 1) {
-            cudaGetLastError();
-            return;
-        }
+        auto resident = [&](auto kernel, int cols, int size) {
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3((unsigned)(d.sms / size * size));
+            cfg.blockDim = dim3(kThreads);
+            cfg.dynamicSmemBytes = (size_t)smem_bytes(cols, cols == 256 ? 1 : size, kMaxGroups);
+            cudaLaunchAttribute la;
+            la.id = cudaLaunchAttributeClusterDimension;
+            la.val.clusterDim.x = (unsigned)size;
+            la.val.clusterDim.y = la.val.clusterDim.z = 1;
+            cfg.attrs = &la;
+            cfg.numAttrs = 1;
+            int n = 0;
+            if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448 - 4096) != cudaSuccess ||
+                cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+                cudaGetLastError();
+                return 0;
+            }
+            return n;
+        };
+        d.pairs = resident(harp_gemm_kernel<false, 256, FORWARD, __nv_bfloat16>, 256, 2);
+        // (the query counts one CTA an SM wherever tensor memory is used; two of these fit, and run)
+        for (int i = 0; i < 3; ++i) d.clusters[i] = 2 * resident(harp_gemm_kernel<false, 32, FORWARD, __nv_bfloat16>, 32, 1 << i);
+        if (d.pairs < 1 || d.clusters[0] < 1) return;
         table[dev] = d;
     });
     return table[dev].err ? &table[dev] : nullptr;
@@ -596,13 +697,11 @@ harp_status_t gemm(const Call &c, const Device &dev, cudaStream_t stream) {
     P.cols = (int32_t)c.d_out;
     P.depth = (int32_t)(c.product == FORWARD ? c.d_in : c.d_out);
     P.pairs = reinterpret_cast<uintptr_t>(c.out) % 4 == 0 && c.ld_out % 2 == 0 && P.lanes % 2 == 0 && !c.accumulate;
-    P.tile_cols = 256;
-    P.split = 1;
-    int64_t tiles;
-    if (c.product == GRAD_WEIGHTS) tiles = (int64_t)c.n_groups * ((P.lanes + 255) / 256) * ((P.cols + 255) / 256);
-    else tiles = ((int64_t)P.lanes + 255) / 256 * ((c.n_rows + 255) / 256 + c.n_groups - 1);
-    if (tiles > INT32_MAX / 2) return HARP_ERR_TOO_LARGE;
-    const int clusters = (int)std::min<int64_t>(tiles, dev.pairs);
+    const Shape shape = choose(c, dev);
+    if (shape.tiles > INT32_MAX / 16) return HARP_ERR_TOO_LARGE;
+    P.tile_cols = shape.cols;
+    P.split = shape.split;
+    const int clusters = (int)std::min<int64_t>(shape.tiles, shape.slots);
 
     // A matrix whose width is a multiple of 64 is also a stack of chunks 64 wide: one copy then brings two of them, which an MN-major
     // operand keeps one behind the other (weight gradients of 8192 rows, 8192 x 8192, two copies a stage instead of four: 897 -> 815 us)
@@ -636,10 +735,11 @@ harp_status_t gemm(const Call &c, const Device &dev, cudaStream_t stream) {
         ok = ok && encode(&maps[1], c.i8, c.rows, 2, e, p, box) && encode(&maps[2], c.i8, c.rows, 2, e, p, box_small);
     }
     if (!ok) return HARP_ERR_UNSUPPORTED;
-    if (c.i8) return launch<true, 2, FORWARD>(c.out_dtype, maps, P, clusters, stream);
-    if (c.product == FORWARD) return launch<false, 2, FORWARD>(c.out_dtype, maps, P, clusters, stream);
-    if (c.product == GRAD_ROWS) return launch<false, 2, GRAD_ROWS>(c.out_dtype, maps, P, clusters, stream);
-    return launch<false, 2, GRAD_WEIGHTS>(c.out_dtype, maps, P, clusters, stream);
+    if (c.product == GRAD_WEIGHTS) return launch<false, 256, GRAD_WEIGHTS>(c.out_dtype, maps, P, clusters, stream);
+    if (c.product == GRAD_ROWS) return launch<false, 256, GRAD_ROWS>(c.out_dtype, maps, P, clusters, stream);
+    if (shape.cols == 32) return c.i8 ? launch<true, 32, FORWARD>(c.out_dtype, maps, P, clusters, stream) : launch<false, 32, FORWARD>(c.out_dtype, maps, P, clusters, stream);
+    if (shape.cols == 64) return c.i8 ? launch<true, 64, FORWARD>(c.out_dtype, maps, P, clusters, stream) : launch<false, 64, FORWARD>(c.out_dtype, maps, P, clusters, stream);
+    return c.i8 ? launch<true, 256, FORWARD>(c.out_dtype, maps, P, clusters, stream) : launch<false, 256, FORWARD>(c.out_dtype, maps, P, clusters, stream);
 }
 
 }  // namespace harp_linear

@@ -1,5 +1,5 @@
-// Declarations shared by the translation units of the layer products (harp_linear.cu: entry points, harp_gemm.cu and
-// harp_gemm_small.cu: kernels, harp_quantize.cu: rows to 8 bits).
+// Declarations shared by the translation units of the layer products (harp_linear.cu: entry points, harp_gemm.cu: the
+// kernel, harp_quantize.cu: rows to 8 bits).
 #pragma once
 
 #include <cuda_runtime.h>
@@ -36,6 +36,7 @@ struct Call {
 
 struct Device {
     int sms = 0, pairs = 0;              // SMs; CTA pairs of the product kernel that are resident at once
+    int clusters[3] = {};                // ... clusters of 1, 2 and 4 CTAs that divide the contracted dimension, two CTAs an SM
     int32_t *err = nullptr;              // device word: a wait gave up
 };
 // of the current device; null where the driver or the device cannot run these kernels
