@@ -453,20 +453,23 @@ def shard_rows(n_rows: int, rank: int, world: int):
 # _harpcall.abi3.so instead of ctypes (1.35 us less) where that was built.
 
 _dtype_codes = {}                  # torch dtype -> harp_dtype_t
-_current_device = _raw_stream = _apply_ex = None
+_current_device = _raw_stream = _apply_ex = _i8 = _bf16 = _f32 = _i32 = None
+_quantize_rows = _linear_i8 = _grouped_linear_i8 = _grouped_linear = _grouped_grad_rows = _grouped_grad_weights = None
 
 
-def _without_ctypes(function):
+def _without_ctypes(function, kind="function"):
     """The same function behind a cheaper call; `function` itself in a tree built without CPython's headers."""
     try:
         from . import _harpcall
-    except ImportError:
+        kind = getattr(_harpcall, kind)
+    except (ImportError, AttributeError):
         return function
-    return _harpcall.function(ctypes.cast(function, ctypes.c_void_p).value)
+    return kind(ctypes.cast(function, ctypes.c_void_p).value)
 
 
 def _bind_torch() -> None:
-    global _current_device, _raw_stream, _apply_ex
+    global _current_device, _raw_stream, _apply_ex, _i8, _bf16, _f32, _i32
+    global _quantize_rows, _linear_i8, _grouped_linear_i8, _grouped_linear, _grouped_grad_rows, _grouped_grad_weights
     import torch
     torch.cuda.init()
     _dtype_codes.update({torch.float32: HARP_F32, torch.bfloat16: HARP_BF16})
@@ -474,6 +477,12 @@ def _bind_torch() -> None:
         _current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
     else:
         _current_device, _raw_stream = torch.cuda.current_device, lambda dev: torch.cuda.current_stream(dev).cuda_stream
+    _i8, _bf16, _f32, _i32 = (torch.int8,), (torch.bfloat16,), torch.float32, torch.int32
+    L = lib()
+    _quantize_rows, _linear_i8 = _without_ctypes(L.harp_quantize_rows, "quantize"), _without_ctypes(L.harp_linear_i8, "linear_i8")
+    _grouped_linear_i8 = _without_ctypes(L.harp_grouped_linear_i8, "grouped_linear_i8")
+    _grouped_linear, _grouped_grad_rows = _without_ctypes(L.harp_grouped_linear, "grouped"), _without_ctypes(L.harp_grouped_grad_rows, "grouped")
+    _grouped_grad_weights = _without_ctypes(L.harp_grouped_grad_weights, "grad_weights")
     # last: what the callers test, also those on other threads
     _apply_ex = _without_ctypes(lib().harp_apply_ex)
 
@@ -516,13 +525,14 @@ def _matrix(name, t, dtypes, dim, device):
     """Leading dimension of a tensor of rows; a weight of several groups has them one behind the other."""
     if t.dtype not in dtypes:
         raise TypeError(f"{name}: unsupported dtype {t.dtype}")
-    if t.dim() != dim or t.get_device() != device:
-        raise ValueError(f"{name}: {dim} dimensions on the current device expected, got {tuple(t.shape)} on {t.device}")
+    shape = t.shape
+    if len(shape) != dim or t.get_device() != device:
+        raise ValueError(f"{name}: {dim} dimensions on the current device expected, got {tuple(shape)} on {t.device}")
     if t.is_contiguous():
-        return t.shape[-1]
+        return shape[-1]
     stride = t.stride()
-    ld = stride[-2] if t.shape[-2] > 1 else max(t.shape[-1], stride[-2])
-    if (t.shape[-1] > 1 and stride[-1] != 1) or ld < t.shape[-1] or (dim == 3 and t.shape[0] > 1 and stride[0] != ld * t.shape[1]):
+    ld = stride[-2] if shape[-2] > 1 else max(shape[-1], stride[-2])
+    if (shape[-1] > 1 and stride[-1] != 1) or ld < shape[-1] or (dim == 3 and shape[0] > 1 and stride[0] != ld * shape[1]):
         raise ValueError(f"{name}: rows have to be contiguous and evenly spaced, got strides {stride}")
     return ld
 
@@ -535,10 +545,10 @@ def _vector(name, t, dtype, n, device):
 
 
 def _output(out, shape, dtype, like, device):
-    import torch
     if out is None:
-        out = torch.empty(shape, dtype=dtype or torch.bfloat16, device=like.device)
-    elif dtype is not None and out.dtype is not dtype:
+        import torch
+        return torch.empty(shape, dtype=dtype or torch.bfloat16, device=like.device), shape[-1]
+    if dtype is not None and out.dtype is not dtype:
         raise TypeError(f"out: {dtype} expected, got {out.dtype}")
     if out.shape != shape:
         raise ValueError(f"out: shape {tuple(shape)} expected, got {tuple(out.shape)}")
@@ -547,134 +557,136 @@ def _output(out, shape, dtype, like, device):
 
 def quantize_rows(x, out=None, scale=None):
     """Rows [n, d] (fp32 or bf16) in 8 bits with a scale each: (q int8 [n, d], scale fp32 [n]), x ~ scale[:, None] * q."""
-    import torch
     if _apply_ex is None:
         _bind_torch()
     device = _current_device()
     ld_x = _matrix("x", x, _dtype_codes, 2, device)
     n, d = x.shape
     if out is None:
-        out = torch.empty((n, d), dtype=torch.int8, device=x.device)
-    elif out.shape != x.shape:
-        raise ValueError(f"out: shape {tuple(x.shape)} expected, got {tuple(out.shape)}")
-    ld_q = _matrix("out", out, (torch.int8,), 2, device)
+        out, ld_q = _output(None, (n, d), _i8[0], x, device)
+    else:
+        ld_q = _matrix("out", out, _i8, 2, device)
+        if out.shape != x.shape:
+            raise ValueError(f"out: shape {tuple(x.shape)} expected, got {tuple(out.shape)}")
     if scale is None:
-        scale = torch.empty(n, dtype=torch.float32, device=x.device)
-    _vector("scale", scale, torch.float32, n, device)
-    harp_quantize_rows(x.data_ptr(), ld_x, n, d, _dtype_codes[x.dtype], out.data_ptr(), ld_q, scale.data_ptr(), _raw_stream(device))
+        scale = _output(None, (n,), _f32, x, device)[0]
+    else:
+        _vector("scale", scale, _f32, n, device)
+    st = _quantize_rows(x.data_ptr(), ld_x, n, d, _dtype_codes[x.dtype], out.data_ptr(), ld_q, scale.data_ptr(), _raw_stream(device))
+    if st != HARP_OK:
+        raise HarpError(st, "harp_quantize_rows")
     return out, scale
 
 
 def linear_i8(x, x_scale, w, w_scale, out=None, out_dtype=None):
     """y = (x w^T) x_scale[:, None] w_scale for int8 x [n, d_in] and w [d_out, d_in]; y is bf16 unless `out` or `out_dtype` says fp32."""
-    import torch
     if _apply_ex is None:
         _bind_torch()
     device = _current_device()
-    i8 = (torch.int8,)
-    ld_x, ld_w = _matrix("x", x, i8, 2, device), _matrix("w", w, i8, 2, device)
-    (n, d_in), d_out = x.shape, w.shape[0]
-    if w.shape[1] != d_in:
-        raise ValueError(f"x has rows of {d_in} and w of {w.shape[1]}")
-    _vector("x_scale", x_scale, torch.float32, n, device)
-    _vector("w_scale", w_scale, torch.float32, d_out, device)
+    ld_x, ld_w = _matrix("x", x, _i8, 2, device), _matrix("w", w, _i8, 2, device)
+    (n, d_in), (d_out, d_w) = x.shape, w.shape
+    if d_w != d_in:
+        raise ValueError(f"x has rows of {d_in} and w of {d_w}")
+    _vector("x_scale", x_scale, _f32, n, device)
+    _vector("w_scale", w_scale, _f32, d_out, device)
     out, ld_y = _output(out, (n, d_out), out_dtype, x, device)
-    harp_linear_i8(x.data_ptr(), ld_x, x_scale.data_ptr(), w.data_ptr(), ld_w, w_scale.data_ptr(), n, d_in, d_out, out.data_ptr(), ld_y,
-                   _dtype_codes[out.dtype], _raw_stream(device))
+    st = _linear_i8(x.data_ptr(), ld_x, x_scale.data_ptr(), w.data_ptr(), ld_w, w_scale.data_ptr(), n, d_in, d_out, out.data_ptr(), ld_y,
+                    _dtype_codes[out.dtype], _raw_stream(device))
+    if st != HARP_OK:
+        raise HarpError(st, "harp_linear_i8")
     return out
 
 
 def grouped_linear_i8(x, x_scale, w, w_scale, offsets, out=None, out_dtype=None):
     """linear_i8 with a weight per group of rows: w [groups, d_out, d_in], w_scale [groups, d_out], offsets int32 [groups + 1]."""
-    import torch
     if _apply_ex is None:
         _bind_torch()
     device = _current_device()
-    i8 = (torch.int8,)
-    ld_x, ld_w = _matrix("x", x, i8, 2, device), _matrix("w", w, i8, 3, device)
+    ld_x, ld_w = _matrix("x", x, _i8, 2, device), _matrix("w", w, _i8, 3, device)
     (n, d_in), (groups, d_out, d_w) = x.shape, w.shape
     if d_w != d_in:
         raise ValueError(f"x has rows of {d_in} and w of {d_w}")
-    _vector("x_scale", x_scale, torch.float32, n, device)
-    _vector("w_scale", w_scale, torch.float32, groups * d_out, device)
-    _vector("offsets", offsets, torch.int32, groups + 1, device)
+    _vector("x_scale", x_scale, _f32, n, device)
+    _vector("w_scale", w_scale, _f32, groups * d_out, device)
+    _vector("offsets", offsets, _i32, groups + 1, device)
     out, ld_y = _output(out, (n, d_out), out_dtype, x, device)
-    harp_grouped_linear_i8(x.data_ptr(), ld_x, x_scale.data_ptr(), w.data_ptr(), ld_w, w_scale.data_ptr(), offsets.data_ptr(), groups, n, d_in,
-                           d_out, out.data_ptr(), ld_y, _dtype_codes[out.dtype], _raw_stream(device))
+    st = _grouped_linear_i8(x.data_ptr(), ld_x, x_scale.data_ptr(), w.data_ptr(), ld_w, w_scale.data_ptr(), offsets.data_ptr(), groups, n, d_in,
+                            d_out, out.data_ptr(), ld_y, _dtype_codes[out.dtype], _raw_stream(device))
+    if st != HARP_OK:
+        raise HarpError(st, "harp_grouped_linear_i8")
     return out
 
 
 def grouped_linear(x, w, offsets, out=None, out_dtype=None):
     """y_r = x_r w_e^T for offsets[e] <= r < offsets[e + 1]: bf16 x [n, d_in], w [groups, d_out, d_in], offsets int32 [groups + 1] on the
     GPU; y is bf16 unless `out` or `out_dtype` says fp32.  Rows outside every group are not written."""
-    import torch
     if _apply_ex is None:
         _bind_torch()
     device = _current_device()
-    bf16 = (torch.bfloat16,)
-    ld_x, ld_w = _matrix("x", x, bf16, 2, device), _matrix("w", w, bf16, 3, device)
+    ld_x, ld_w = _matrix("x", x, _bf16, 2, device), _matrix("w", w, _bf16, 3, device)
     (n, d_in), (groups, d_out, d_w) = x.shape, w.shape
     if d_w != d_in:
         raise ValueError(f"x has rows of {d_in} and w of {d_w}")
-    _vector("offsets", offsets, torch.int32, groups + 1, device)
+    _vector("offsets", offsets, _i32, groups + 1, device)
     out, ld_y = _output(out, (n, d_out), out_dtype, x, device)
-    harp_grouped_linear(x.data_ptr(), ld_x, w.data_ptr(), ld_w, offsets.data_ptr(), groups, n, d_in, d_out, out.data_ptr(), ld_y,
-                        _dtype_codes[out.dtype], _raw_stream(device))
+    st = _grouped_linear(x.data_ptr(), ld_x, w.data_ptr(), ld_w, offsets.data_ptr(), groups, n, d_in, d_out, out.data_ptr(), ld_y,
+                         _dtype_codes[out.dtype], _raw_stream(device))
+    if st != HARP_OK:
+        raise HarpError(st, "harp_grouped_linear")
     return out
 
 
 def grouped_grad_rows(gy, w, offsets, out=None, out_dtype=None):
     """Gradient of grouped_linear with respect to its rows: gx_r = gy_r w_e."""
-    import torch
     if _apply_ex is None:
         _bind_torch()
     device = _current_device()
-    bf16 = (torch.bfloat16,)
-    ld_gy, ld_w = _matrix("gy", gy, bf16, 2, device), _matrix("w", w, bf16, 3, device)
+    ld_gy, ld_w = _matrix("gy", gy, _bf16, 2, device), _matrix("w", w, _bf16, 3, device)
     (n, d_gy), (groups, d_out, d_in) = gy.shape, w.shape
     if d_gy != d_out:
         raise ValueError(f"gy has rows of {d_gy} and w {d_out} rows")
-    _vector("offsets", offsets, torch.int32, groups + 1, device)
+    _vector("offsets", offsets, _i32, groups + 1, device)
     out, ld_gx = _output(out, (n, d_in), out_dtype, gy, device)
-    harp_grouped_grad_rows(gy.data_ptr(), ld_gy, w.data_ptr(), ld_w, offsets.data_ptr(), groups, n, d_in, d_out, out.data_ptr(), ld_gx,
-                           _dtype_codes[out.dtype], _raw_stream(device))
+    st = _grouped_grad_rows(gy.data_ptr(), ld_gy, w.data_ptr(), ld_w, offsets.data_ptr(), groups, n, d_in, d_out, out.data_ptr(), ld_gx,
+                            _dtype_codes[out.dtype], _raw_stream(device))
+    if st != HARP_OK:
+        raise HarpError(st, "harp_grouped_grad_rows")
     return out
 
 
 def grouped_grad_weights(gy, x, offsets, out=None, out_dtype=None, accumulate=False):
     """Gradient of grouped_linear with respect to its weights: gw_e = sum of gy_r^T x_r over the rows of e, [groups, d_out, d_in], fp32
     unless `out` or `out_dtype` says bf16; added to `out` with accumulate."""
-    import torch
     if _apply_ex is None:
         _bind_torch()
     device = _current_device()
-    bf16 = (torch.bfloat16,)
-    ld_gy, ld_x = _matrix("gy", gy, bf16, 2, device), _matrix("x", x, bf16, 2, device)
+    ld_gy, ld_x = _matrix("gy", gy, _bf16, 2, device), _matrix("x", x, _bf16, 2, device)
     (n, d_out), (n_x, d_in), groups = gy.shape, x.shape, offsets.numel() - 1
     if n != n_x:
         raise ValueError(f"gy has {n} rows and x {n_x}")
     if accumulate and out is None:
         raise ValueError("accumulate needs out")
-    _vector("offsets", offsets, torch.int32, groups + 1, device)
-    out, ld_gw = _output(out, (groups, d_out, d_in), out_dtype or (torch.float32 if out is None else None), gy, device)
-    harp_grouped_grad_weights(gy.data_ptr(), ld_gy, x.data_ptr(), ld_x, offsets.data_ptr(), groups, n, d_in, d_out, out.data_ptr(), ld_gw,
-                              _dtype_codes[out.dtype], accumulate, _raw_stream(device))
+    _vector("offsets", offsets, _i32, groups + 1, device)
+    out, ld_gw = _output(out, (groups, d_out, d_in), out_dtype or (_f32 if out is None else None), gy, device)
+    st = _grouped_grad_weights(gy.data_ptr(), ld_gy, x.data_ptr(), ld_x, offsets.data_ptr(), groups, n, d_in, d_out, out.data_ptr(), ld_gw,
+                               _dtype_codes[out.dtype], 1 if accumulate else 0, _raw_stream(device))
+    if st != HARP_OK:
+        raise HarpError(st, "harp_grouped_grad_weights")
     return out
 
 
 def processed_linear_i8(x, plan_in: Plan, plan_out: Plan, w, w_scale, out=None, scratch=None):
     """A processed layer in 8 bits, y = (x Q_in) W~^T Q_out^T: contiguous rows x [n, plan_in.d] (fp32 or bf16; overwritten with x Q_in), W~ as
     quantize_rows gave it.  `scratch`: contiguous, harp_processed_linear_scratch_bytes(plan_in, n) bytes at least."""
-    import torch
     if _apply_ex is None:
         _bind_torch()
     device = _current_device()
     _matrix("x", x, _dtype_codes, 2, device)
-    ld_w = _matrix("w", w, (torch.int8,), 2, device)
+    ld_w = _matrix("w", w, _i8, 2, device)
     n = x.shape[0]
     if not x.is_contiguous() or x.shape[1] != plan_in.d or w.shape != (plan_out.d, plan_in.d):
         raise ValueError(f"contiguous rows of {plan_in.d} and a weight {(plan_out.d, plan_in.d)} expected, got {tuple(x.shape)} and {tuple(w.shape)}")
-    _vector("w_scale", w_scale, torch.float32, plan_out.d, device)
+    _vector("w_scale", w_scale, _f32, plan_out.d, device)
     out, _ = _output(out, (n, plan_out.d), x.dtype, x, device)
     if not out.is_contiguous():
         raise ValueError("out has to be contiguous")
