@@ -23,6 +23,7 @@
 #include <algorithm>
 #include <cmath>
 #include <mutex>
+#include <type_traits>
 
 #include <cuda.h>
 
@@ -37,7 +38,6 @@ using namespace harp_gemm_ptx;
 
 constexpr int kThreads = 384;                // warps: 0 copies, 1 products, 2 tensor memory and ragged ends, 3 offsets, 4-11 epilogue (two a lane quarter)
 constexpr int kHalf = 16384;                 // the lane operand's part of a stage in one CTA
-constexpr int kPrefetch = 8;                 // blocks of a weight that one CTA asks for before its turn
 constexpr int kSumCols = 32;                 // columns whose sums a split adds up at a time
 // COLS: most columns of a tile (256 for a pair of CTAs, 32 or 64 for one)
 __host__ __device__ constexpr int stage_bytes(int cols) { return kHalf + (cols == 256 ? 128 : cols) * 128; }
@@ -256,12 +256,6 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     if (size > 1) cluster_sync();
     else __syncthreads();
     tc_fence_after();
-    if (CG == 1 && PRODUCT == FORWARD && P.offsets == nullptr && warp == 0 && lane == 0 && cluster < first[1]) {
-        // The first blocks of the weight, into L2: whatever the kernels before this one still write, L2 is where it meets.
-        const Tile T = tile_at<CG, PRODUCT, BLOCK>(cluster, P, off, first);
-        const int b0 = (int)((int64_t)T.blocks * (int)rank / P.split), b1 = (int)((int64_t)T.blocks * ((int)rank + 1) / P.split);
-        for (int b = b0; b < min(b1, b0 + kPrefetch); ++b) prefetch_3d(&map_a, b * BLOCK, T.lane0, 0);
-    }
     wait_for_previous();
     launch_dependents();
     if (P.offsets) {
@@ -371,9 +365,13 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 phases ^= 1u << ring.s;
                 if (!wait(ragged(ring.s), phase, 4)) break;
                 const int chunks = 2 + div_up(width(T) / CG, 64);    // of 64 lanes or columns, 64 rows of 128 bytes each
+                unsigned char *const stage = base_ptr + ring.s * kStage + (lane & 7) * 16;
                 for (int c = 0; c < chunks; ++c)
-                    for (int r = T.tail; r < round_up(T.tail, 16); ++r)
-                        *reinterpret_cast<uint32_t *>(base_ptr + ring.s * kStage + c * 8192 + r * 128 + lane * 4) = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {                    // four rows at a time
+                        const int r = (T.tail & ~15) + i * 4 + (lane >> 3);
+                        if (r >= T.tail) *reinterpret_cast<uint4 *>(stage + c * 8192 + r * 128) = make_uint4(0, 0, 0, 0);
+                    }
                 fence_async_smem();
                 __syncwarp();
                 if (CG == 2 && rank == 1) {
@@ -441,24 +439,43 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                             v[j + 3] = __float_as_uint((float)(int32_t)v[j + 3] * by_lane * r.w);
                         }
                     }
+                    // A whole chunk goes without a test a column: with one, 18 instructions a store kept 64 x 128 rows, 2048 x 1024
+                    // (fp32 weight gradients) at 259 us, 117 now.
+                    const int left = T.cols - c0;
                     if (pairs) {
                         // neighbouring lanes trade halves of two columns: either then stores both lanes' elements of one
                         const int odd = lane & 1;
-                        Out *p = out - odd + (int64_t)(c0 + odd) * P.ld_out;
-                        const int left = inside ? T.cols - c0 - odd : 0;
 #pragma unroll
                         for (int j = 0; j < 32; j += 2) {
                             const uint32_t got = __shfl_xor_sync(~0u, odd ? v[j] : v[j + 1], 1);
-                            const uint32_t both = pack_bf16(odd ? got : v[j], odd ? v[j + 1] : got);
-                            if (j < left) *reinterpret_cast<uint32_t *>(p) = both;
-                            p += 2 * P.ld_out;
+                            v[j] = pack_bf16(odd ? got : v[j], odd ? v[j + 1] : got);
+                        }
+                        if (inside) {
+                            Out *p = out - odd + (int64_t)(c0 + odd) * P.ld_out;
+                            const int64_t step = 2 * P.ld_out;
+                            if (left >= 32) {
+#pragma unroll
+                                for (int j = 0; j < 32; j += 2, p += step) *reinterpret_cast<uint32_t *>(p) = v[j];
+                            } else {
+#pragma unroll
+                                for (int j = 0; j < 32; j += 2, p += step)
+                                    if (j + odd < left) *reinterpret_cast<uint32_t *>(p) = v[j];
+                            }
                         }
                     } else if (inside) {
                         Out *p = out + (int64_t)c0 * P.ld_out;
+                        if (PRODUCT == GRAD_WEIGHTS && P.accumulate) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            if (c0 + j < T.cols) store(p, __uint_as_float(v[j]) + (PRODUCT == GRAD_WEIGHTS && P.accumulate ? load(p) : 0.0f));
-                            p += P.ld_out;
+                            for (int j = 0; j < 32; ++j)
+                                if (j < left) v[j] = __float_as_uint(__uint_as_float(v[j]) + load(p + (int64_t)j * P.ld_out));
+                        }
+                        if (left >= 32) {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j, p += P.ld_out) store(p, __uint_as_float(v[j]));
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j, p += P.ld_out)
+                                if (j < left) store(p, __uint_as_float(v[j]));
                         }
                     }
                 }
@@ -607,10 +624,9 @@ Shape choose(const Call &c, const Device &dev) {
     const int64_t lanes = c.product == FORWARD ? c.d_out : c.d_in, pair_tiles = (lanes + 255) / 256, tiles = (lanes + 127) / 128;
     if (c.product == GRAD_WEIGHTS) return {256, 1, dev.pairs, c.n_groups * pair_tiles * ((c.d_out + 255) / 256)};
     const Shape pairs = {256, 1, dev.pairs, pair_tiles * ((c.n_rows + 255) / 256 + c.n_groups - 1)};
-    if (c.product == GRAD_ROWS) return pairs;
     // rows of a group, and half as many again where there are several: they are not even
     const int64_t met = std::min<int64_t>(c.n_groups, c.n_rows), even = (c.n_rows + met - 1) / met, rows = met > 1 ? even + even / 2 : even;
-    const double blocks = (double)((c.d_in * (c.i8 ? 1 : 2) + 127) / 128), memory = (double)(met * tiles) * blocks * 16384 / 6.3e6;     // us
+    const double blocks = (double)(((c.product == FORWARD ? c.d_in : c.d_out) * (c.i8 ? 1 : 2) + 127) / 128), memory = (double)(met * tiles) * blocks * 16384 / 6.3e6;     // us
     auto cols_of = [&](int most) { return (double)((rows + most - 1) / most); };
     Shape best = pairs;
     double least;
@@ -625,7 +641,7 @@ Shape choose(const Call &c, const Device &dev) {
             const double n = (double)(met * tiles) * cols_of(cols), rounds = std::ceil(n / dev.clusters[i]);
             const double stretch = rounds > 1 ? 0.75 + 0.25 * rounds * dev.clusters[i] / n : 1;
             const double join = i ? (cols == 32 ? 2.5 : 4) : 0.5;        // adding up a tile's sums
-            const double block = n * (1 << i) > dev.sms ? (cols == 32 ? 0.33 : 0.42) : (cols == 32 ? 0.285 : 0.36);
+            const double block = n * (1 << i) > dev.sms ? (cols == 32 ? 0.37 : 0.42) : (cols == 32 ? 0.285 : 0.36);
             const double t = std::max(memory * stretch, rounds * (blocks / (1 << i) * block + join)) + 3.5;
             if (dev.clusters[i] > 0 && t < least) {
                 least = t;
@@ -735,11 +751,16 @@ harp_status_t gemm(const Call &c, const Device &dev, cudaStream_t stream) {
         ok = ok && encode(&maps[1], c.i8, c.rows, 2, e, p, box) && encode(&maps[2], c.i8, c.rows, 2, e, p, box_small);
     }
     if (!ok) return HARP_ERR_UNSUPPORTED;
+    auto by_cols = [&](auto i8, auto product) {
+        constexpr bool I8 = decltype(i8)::value;
+        constexpr int PRODUCT = decltype(product)::value;
+        if (shape.cols == 32) return launch<I8, 32, PRODUCT>(c.out_dtype, maps, P, clusters, stream);
+        if (shape.cols == 64) return launch<I8, 64, PRODUCT>(c.out_dtype, maps, P, clusters, stream);
+        return launch<I8, 256, PRODUCT>(c.out_dtype, maps, P, clusters, stream);
+    };
     if (c.product == GRAD_WEIGHTS) return launch<false, 256, GRAD_WEIGHTS>(c.out_dtype, maps, P, clusters, stream);
-    if (c.product == GRAD_ROWS) return launch<false, 256, GRAD_ROWS>(c.out_dtype, maps, P, clusters, stream);
-    if (shape.cols == 32) return c.i8 ? launch<true, 32, FORWARD>(c.out_dtype, maps, P, clusters, stream) : launch<false, 32, FORWARD>(c.out_dtype, maps, P, clusters, stream);
-    if (shape.cols == 64) return c.i8 ? launch<true, 64, FORWARD>(c.out_dtype, maps, P, clusters, stream) : launch<false, 64, FORWARD>(c.out_dtype, maps, P, clusters, stream);
-    return c.i8 ? launch<true, 256, FORWARD>(c.out_dtype, maps, P, clusters, stream) : launch<false, 256, FORWARD>(c.out_dtype, maps, P, clusters, stream);
+    if (c.product == GRAD_ROWS) return by_cols(std::false_type(), std::integral_constant<int, GRAD_ROWS>());
+    return c.i8 ? by_cols(std::true_type(), std::integral_constant<int, FORWARD>()) : by_cols(std::false_type(), std::integral_constant<int, FORWARD>());
 }
 
 }  // namespace harp_linear

@@ -64,10 +64,6 @@ __device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap *map, in
                      ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
 
-// into L2 alone
-__device__ __forceinline__ void prefetch_3d(const CUtensorMap *map, int x, int y, int z) {
-    asm volatile("cp.async.bulk.prefetch.tensor.3d.L2.global.tile [%0, {%1, %2, %3}];" ::"l"(map), "r"(x), "r"(y), "r"(z) : "memory");
-}
 template <int CG>
 __device__ __forceinline__ void load_4d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int w, uint32_t bar) {
     if (CG == 1) tma_load_4d(dst, map, x, y, z, w, bar);
