@@ -21,6 +21,7 @@
 // along the columns; in GRAD_WEIGHTS a warp overwrites them with zeros before the products, in both
 // operands, because the other group's values may be infinite.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <mutex>
 #include <type_traits>
@@ -43,6 +44,7 @@ constexpr int kSumCols = 32;                 // columns whose sums a split adds 
 __host__ __device__ constexpr int stage_bytes(int cols) { return kHalf + (cols == 256 ? 128 : cols) * 128; }
 __host__ __device__ constexpr int stages(int cols) { return cols == 256 ? 6 : cols == 64 ? 3 : 4; }      // one CTA leaves room for another one
 constexpr uint32_t kSpin = 1u << 22;         // limit of every wait
+constexpr int kMostSmem = 232448 - 4096;     // dynamic shared memory, less what the kernels have besides
 
 __device__ int32_t g_gemm_err;
 
@@ -573,7 +575,7 @@ int smem_bytes(int cols, int split, int n_groups) {
 template <bool I8, int COLS, int PRODUCT, typename Out>
 harp_status_t launch(const CUtensorMap (&maps)[3], const Params &P, int clusters, cudaStream_t s) {
     const auto kernel = harp_gemm_kernel<I8, COLS, PRODUCT, Out>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448 - 4096) != cudaSuccess) return HARP_ERR_CUDA;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem) != cudaSuccess) return HARP_ERR_CUDA;
     const int size = COLS == 256 ? 2 : P.split;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(clusters * size));
@@ -643,7 +645,7 @@ Shape choose(const Call &c, const Device &dev) {
             const double join = i ? (cols == 32 ? 2.5 : 4) : 0.5;        // adding up a tile's sums
             const double block = n * (1 << i) > dev.sms ? (cols == 32 ? 0.37 : 0.42) : (cols == 32 ? 0.285 : 0.36);
             const double t = std::max(memory * stretch, rounds * (blocks / (1 << i) * block + join)) + 3.5;
-            if (dev.clusters[i] > 0 && t < least) {
+            if (t < least) {
                 least = t;
                 best = {cols, 1 << i, dev.clusters[i], tiles * ((c.n_rows + cols - 1) / cols + c.n_groups - 1)};
             }
@@ -653,47 +655,59 @@ Shape choose(const Call &c, const Device &dev) {
 
 }  // namespace
 
+namespace {
+
+bool describe(int dev, Device &d) {
+    void *err = nullptr;
+    if (!harp_tensor_map_encoder(nullptr) || cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+        cudaGetSymbolAddress(&err, g_gemm_err) != cudaSuccess)
+        return false;
+    auto resident = [&](auto kernel, int cols, int size) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)(d.sms / size * size));
+        cfg.blockDim = dim3(kThreads);
+        cfg.dynamicSmemBytes = (size_t)smem_bytes(cols, cols == 256 ? 1 : size, kMaxGroups);
+        cudaLaunchAttribute la;
+        la.id = cudaLaunchAttributeClusterDimension;
+        la.val.clusterDim.x = (unsigned)size;
+        la.val.clusterDim.y = la.val.clusterDim.z = 1;
+        cfg.attrs = &la;
+        cfg.numAttrs = 1;
+        int n = 0;
+        const bool ok = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem) == cudaSuccess &&
+                        cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess;
+        return ok ? n : 0;
+    };
+    d.pairs = resident(harp_gemm_kernel<false, 256, FORWARD, __nv_bfloat16>, 256, 2);
+    // (the query counts one CTA an SM wherever tensor memory is used; two of these fit, and run)
+    for (int i = 0; i < 3; ++i) d.clusters[i] = 2 * resident(harp_gemm_kernel<false, 32, FORWARD, __nv_bfloat16>, 32, 1 << i);
+    d.err = static_cast<int32_t *>(err);
+    return d.pairs > 0 && d.clusters[0] > 0 && d.clusters[1] > 0 && d.clusters[2] > 0;
+}
+
+}  // namespace
+
 const Device *device() {
     constexpr int kMost = 64;
     static Device table[kMost];
-    static std::once_flag once[kMost];
+    static std::atomic<bool> known[kMost];
+    static std::mutex mu;
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMost) return nullptr;
-    std::call_once(once[dev], [dev] {
-        Device d;
-        void *err = nullptr;
-        if (!harp_tensor_map_encoder(nullptr) || cudaDeviceGetAttribute(&d.sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
-            cudaGetSymbolAddress(&err, g_gemm_err) != cudaSuccess) {
-            cudaGetLastError();
-            return;
-        }
-        d.err = static_cast<int32_t *>(err);
-        auto resident = [&](auto kernel, int cols, int size) {
-            cudaLaunchConfig_t cfg = {};
-            cfg.gridDim = dim3((unsigned)(d.sms / size * size));
-            cfg.blockDim = dim3(kThreads);
-            cfg.dynamicSmemBytes = (size_t)smem_bytes(cols, cols == 256 ? 1 : size, kMaxGroups);
-            cudaLaunchAttribute la;
-            la.id = cudaLaunchAttributeClusterDimension;
-            la.val.clusterDim.x = (unsigned)size;
-            la.val.clusterDim.y = la.val.clusterDim.z = 1;
-            cfg.attrs = &la;
-            cfg.numAttrs = 1;
-            int n = 0;
-            if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448 - 4096) != cudaSuccess ||
-                cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
-                cudaGetLastError();
-                return 0;
-            }
-            return n;
-        };
-        d.pairs = resident(harp_gemm_kernel<false, 256, FORWARD, __nv_bfloat16>, 256, 2);
-        // (the query counts one CTA an SM wherever tensor memory is used; two of these fit, and run)
-        for (int i = 0; i < 3; ++i) d.clusters[i] = 2 * resident(harp_gemm_kernel<false, 32, FORWARD, __nv_bfloat16>, 32, 1 << i);
-        if (d.pairs < 1 || d.clusters[0] < 1) return;
-        table[dev] = d;
-    });
-    return table[dev].err ? &table[dev] : nullptr;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMost) {
+        cudaGetLastError();
+        return nullptr;
+    }
+    if (known[dev].load(std::memory_order_acquire)) return &table[dev];
+    std::lock_guard<std::mutex> lock(mu);
+    if (known[dev].load(std::memory_order_relaxed)) return &table[dev];
+    Device d;
+    if (!describe(dev, d)) {             // asked again at the next call
+        cudaGetLastError();
+        return nullptr;
+    }
+    table[dev] = d;
+    known[dev].store(true, std::memory_order_release);
+    return &table[dev];
 }
 
 harp_status_t gemm(const Call &c, const Device &dev, cudaStream_t stream) {
