@@ -39,6 +39,10 @@ using namespace harp_gemm_ptx;
 
 constexpr int kThreads = 384;                // warps: 0 copies, 1 products, 2 tensor memory and ragged ends, 3 offsets, 4-11 epilogue (two a lane quarter)
 constexpr int kHalf = 16384;                 // the lane operand's part of a stage in one CTA
+// The tensor core cuts its fp32 sums off instead of rounding them, sixteen products at a time: the result of a long sum is too small by
+// 1.1e-9 of itself a product (1.6e-5 after 14336).  Results in fp32 are therefore summed in runs of 512 products, which the epilogue adds up,
+// rounding to nearest: 5e-7 at any length.  bf16 results round off 2^-9 in any case and take one run.
+constexpr int kRun = 8;                      // blocks
 constexpr int kSumCols = 32;                 // columns whose sums a split adds up at a time
 // COLS: most columns of a tile (256 for a pair of CTAs, 32 or 64 for one)
 __host__ __device__ constexpr int stage_bytes(int cols) { return kHalf + (cols == 256 ? 128 : cols) * 128; }
@@ -174,6 +178,8 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     constexpr int CG = COLS == 256 ? 2 : 1;                  // CTAs a tile
     constexpr int STAGES = stages(COLS), kStage = stage_bytes(COLS);
     constexpr bool A_MN = PRODUCT != FORWARD, B_MN = PRODUCT == GRAD_WEIGHTS;
+    constexpr bool RUNS = !I8 && sizeof(Out) == 4;           // sums of runs of blocks are added up in registers
+    constexpr int RUN = RUNS ? kRun : 1 << 30;
     constexpr uint32_t COLUMNS = 2 * COLS, ACC = COLS;       // two accumulators
 
     extern __shared__ unsigned char smem_raw[];
@@ -328,31 +334,31 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         bool alive = true;
         for (int t = cluster; alive && t < n_tiles; t += clusters) {
             const Tile T = at(t);
-            const int b0 = from(T), b1 = to(T);
-            if (T.blocks == 0) continue;
+            const int b1 = to(T);
             const uint32_t idesc = instr(I8, A_MN, B_MN, 128 * CG, width(T));
-            const int acc = n & 1;
-            if (!wait(taken(acc), ((n >> 1) & 1) ^ 1, 2)) break;
-            tc_fence_after();
-            const uint32_t d = columns + acc * ACC;
-            for (int b = b0; b < b1; ++b, ring.next()) {
-                const int s = ring.s;
-                if (!wait(full(s), ring.phase, 3)) { alive = false; break; }
+            for (int b = from(T); alive && b < b1; ++n) {
+                const int acc = n & 1, start = b, stop = min(b1, b + RUN);
+                if (!wait(taken(acc), ((n >> 1) & 1) ^ 1, 2)) { alive = false; break; }
                 tc_fence_after();
-                const uint32_t a = base + (uint32_t)s * kStage;
-                const uint64_t da = A_MN ? operand(a, 8192, 1024) : operand(a, 16, 1024);
-                const uint64_t db = B_MN ? operand(a + kHalf, 8192, 1024) : operand(a + kHalf, 16, 1024);
-                constexpr uint64_t step_a = A_MN ? 128 : 2, step_b = B_MN ? 128 : 2;
-                if (PRODUCT == GRAD_WEIGHTS && b == T.blocks - 1) {
-                    for (int k = 0; k < div_up(T.tail, 16); ++k) mma_ss<I8, CG>(d, da + step_a * k, db + step_b * k, idesc, b > b0 || k > 0);
-                } else {
+                const uint32_t d = columns + acc * ACC;
+                for (; b < stop; ++b, ring.next()) {
+                    const int s = ring.s;
+                    if (!wait(full(s), ring.phase, 3)) { alive = false; break; }
+                    tc_fence_after();
+                    const uint32_t a = base + (uint32_t)s * kStage;
+                    const uint64_t da = A_MN ? operand(a, 8192, 1024) : operand(a, 16, 1024);
+                    const uint64_t db = B_MN ? operand(a + kHalf, 8192, 1024) : operand(a + kHalf, 16, 1024);
+                    constexpr uint64_t step_a = A_MN ? 128 : 2, step_b = B_MN ? 128 : 2;
+                    if (PRODUCT == GRAD_WEIGHTS && b == T.blocks - 1) {
+                        for (int k = 0; k < div_up(T.tail, 16); ++k) mma_ss<I8, CG>(d, da + step_a * k, db + step_b * k, idesc, b > start || k > 0);
+                    } else {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) mma_ss<I8, CG>(d, da + step_a * k, db + step_b * k, idesc, b > b0 || k > 0);
+                        for (int k = 0; k < 4; ++k) mma_ss<I8, CG>(d, da + step_a * k, db + step_b * k, idesc, b > start || k > 0);
+                    }
+                    commit<CG>(empty(s));
                 }
-                commit<CG>(empty(s));
+                if (alive) commit<CG>(done(acc));
             }
-            if (alive && b1 > b0) commit<CG>(done(acc));
-            ++n;
         }
     } else if (warp == 2 && PRODUCT == GRAD_WEIGHTS) {
         // the other groups' rows of a ragged last block
@@ -402,8 +408,8 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     for (int c = part; c < T.cols; c += 2) store(out + (int64_t)c * P.ld_out, 0.0f);
                 continue;
             }
-            const int acc = n & 1;
-            const bool any = to(T) > from(T);
+            const int blocks = to(T) - from(T);
+            const bool any = blocks > 0;                     // ranks of a split may have none
             float by_row[COLS / 64 ? COLS / 64 : 1];         // 8 bits: the rows' scales of this warp's chunks, a lane's column of each
             if (I8 && (CG == 2 || P.split == 1)) {
 #pragma unroll
@@ -412,24 +418,61 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     by_row[i] = c < T.cols ? P.row_scale[T.row0 + c] : 0.0f;
                 }
             }
-            if (any && !wait(done(acc), (n >> 1) & 1, 5)) break;
-            tc_fence_after();
-            const uint32_t d = columns + acc * ACC + ((uint32_t)q << 21);
             const int w = width(T);
-            if (CG == 2 || P.split == 1) {
+            const bool whole = CG == 2 || P.split == 1;
+            // the accumulator that is to be read next; and what it takes to hand it back
+            auto accumulator = [&] { return columns + (n & 1) * ACC + ((uint32_t)q << 21); };
+            auto arrived = [&] {
+                if (!wait(done(n & 1), (n >> 1) & 1, 5)) return false;
+                tc_fence_after();
+                return true;
+            };
+            auto hand_back = [&] {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_at(CG == 2 ? map_rank(taken(n & 1), 0) : taken(n & 1));
+                ++n;
+            };
+            // this warp's columns: chunks of 32, or of 16 out of 32 where sums are divided among ranks
+            float held[RUNS ? (COLS == 256 ? 128 : 32) : 1];
+            if (RUNS) {
+#pragma unroll
+                for (int i = 0; i < (int)(sizeof held / sizeof held[0]); ++i) held[i] = 0.0f;
+                for (int r = 0; r < blocks; r += RUN) {
+                    if (!arrived()) { alive = false; break; }
+#pragma unroll
+                    for (int i = 0; i < (int)(sizeof held / sizeof held[0]) / 16; ++i) {
+                        const int c0 = whole ? (i & ~1) * 32 + part * 32 + (i & 1) * 16 : i * 32 + part * 16;
+                        if (c0 < w) {
+                            uint32_t v[16];
+                            tmem_ld16(accumulator() + c0, v);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) held[i * 16 + j] += __uint_as_float(v[j]);
+                        }
+                    }
+                    hand_back();
+                }
+                if (!alive) break;
+            } else if (any && !arrived()) break;
+            const uint32_t d = accumulator();
+            if (whole) {
                 const bool pairs = sizeof(Out) == 2 && P.pairs;
 #pragma unroll
                 for (int i = 0; i < (int)(sizeof by_row / sizeof by_row[0]); ++i) {
                     const int c0 = (2 * i + part) * 32;
                     if (c0 >= w) break;
                     uint32_t v[32];
-                    tmem_ld32(d + c0, v);
+                    if (RUNS) {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(held[(i * 32 + j) % (sizeof held / sizeof held[0])]);
+                    } else tmem_ld32(d + c0, v);
                     if (I8) {
                         __syncwarp();
                         s_scale[warp - 4][lane] = by_row[i];
                         __syncwarp();
                     }
-                    tmem_wait_ld();
+                    if (!RUNS) tmem_wait_ld();
                     if (I8) {
                         const float4 *const scale = reinterpret_cast<const float4 *>(s_scale[warp - 4]);
 #pragma unroll
@@ -483,14 +526,20 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 }
             } else {
                 // 32 columns at a time, dealt out to the ranks in runs of 4 to 16; sums[source][four columns of the run][lane][4]
-                for (int h = 0; h < w; h += kSumCols, sums_phase ^= 1) {
+#pragma unroll
+                for (int i = 0; i < COLS / kSumCols; ++i) {
+                    const int h = i * kSumCols;
+                    if (h >= w) break;
                     const int run = min(w - h, kSumCols) / P.split, shift = 31 - __clz(run);       // powers of two, as 16, 32 and the split are
                     if (threadIdx.x == 128) mbar_expect_tx(sums_full, (uint32_t)(P.split * run * 512));
                     if (!wait(sums_free, sums_phase ^ 1, 6)) { alive = false; break; }
                     const int c0 = h + part * 16;
                     if (c0 < w) {
                         uint32_t v[16];
-                        if (any) {
+                        if (RUNS) {
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) v[j] = __float_as_uint(held[(i * 16 + j) % (sizeof held / sizeof held[0])]);
+                        } else if (any) {
                             tmem_ld16(d + c0, v);
                             tmem_wait_ld();
                         }
@@ -506,8 +555,8 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     const uint4 *const mine = reinterpret_cast<const uint4 *>(base_ptr + STAGES * kStage) + q * 32 + lane;
                     float x[2][4];                           // this warp's columns: every other four of at most sixteen
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int c = (2 * i + part) * 4;
+                    for (int g = 0; g < 2; ++g) {
+                        const int c = (2 * g + part) * 4;
                         if (c < run) {
                             uint4 sum = make_uint4(0, 0, 0, 0);
                             for (int r = 0; r < P.split; ++r) {
@@ -515,29 +564,27 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                                 if (I8) sum.x += s.x, sum.y += s.y, sum.z += s.z, sum.w += s.w;
                                 else sum.x = add(sum.x, s.x), sum.y = add(sum.y, s.y), sum.z = add(sum.z, s.z), sum.w = add(sum.w, s.w);
                             }
-                            x[i][0] = I8 ? (float)(int32_t)sum.x : __uint_as_float(sum.x);
-                            x[i][1] = I8 ? (float)(int32_t)sum.y : __uint_as_float(sum.y);
-                            x[i][2] = I8 ? (float)(int32_t)sum.z : __uint_as_float(sum.z);
-                            x[i][3] = I8 ? (float)(int32_t)sum.w : __uint_as_float(sum.w);
+                            x[g][0] = I8 ? (float)(int32_t)sum.x : __uint_as_float(sum.x);
+                            x[g][1] = I8 ? (float)(int32_t)sum.y : __uint_as_float(sum.y);
+                            x[g][2] = I8 ? (float)(int32_t)sum.z : __uint_as_float(sum.z);
+                            x[g][3] = I8 ? (float)(int32_t)sum.w : __uint_as_float(sum.w);
                         }
                     }
                     __syncwarp();
                     if (lane < P.split) mbar_arrive_at(map_rank(sums_free, lane));
 #pragma unroll
-                    for (int i = 0; i < 2; ++i)
+                    for (int g = 0; g < 2; ++g)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            const int c = (2 * i + part) * 4 + j, col = h + (int)rank * run + c;
+                            const int c = (2 * g + part) * 4 + j, col = h + (int)rank * run + c;
                             if (inside && c < run && col < T.cols)
-                                store(out + (int64_t)col * P.ld_out, I8 ? x[i][j] * by_lane * P.row_scale[T.row0 + col] : x[i][j]);
+                                store(out + (int64_t)col * P.ld_out, I8 ? x[g][j] * by_lane * P.row_scale[T.row0 + col] : x[g][j]);
                         }
+                    sums_phase ^= 1;
                 }
                 if (!alive) break;
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive_at(CG == 2 ? map_rank(taken(acc), 0) : taken(acc));
-            ++n;
+            if (!RUNS && any) hand_back();
         }
     }
     __syncwarp();
