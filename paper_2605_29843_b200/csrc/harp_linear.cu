@@ -14,11 +14,17 @@ constexpr int64_t kMostDepthI8 = 131071;         // 128 * 128 * d_in stays below
 bool aligned(const void *p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 
 // One 16-byte piece of the padded copy a thread; the source is read by the aligned words that hold the bytes of the piece, which
-// two neighbours make up a word of the result.
-__global__ void pad_rows_kernel(const uint8_t *__restrict__ src, int64_t pitch, int64_t rows, int64_t bytes, uint4 *__restrict__ dst, int64_t pieces) {
-    const int64_t n = rows * pieces;
-    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
-        const int64_t r = i / pieces, at = (i - r * pieces) * 16;
+// two neighbours make up a word of the result.  Weights (offsets given) are copied for the groups that have rows; offsets that fall
+// make an empty group whatever they are clamped to.
+__global__ void pad_rows_kernel(const uint8_t *__restrict__ src, int64_t pitch, int64_t rows, int64_t bytes, uint4 *__restrict__ dst, int64_t pieces,
+                                const int32_t *__restrict__ offsets, int64_t group_rows) {
+    const int64_t piece = (int64_t)blockIdx.x * blockDim.x + threadIdx.x, at = piece * 16;
+    if (piece >= pieces) return;
+    for (int64_t r = (int64_t)blockIdx.y * blockDim.y + threadIdx.y; r < rows; r += (int64_t)gridDim.y * blockDim.y) {
+        if (offsets) {
+            const int64_t e = r / group_rows;
+            if (offsets[e + 1] <= offsets[e]) continue;
+        }
         const int64_t left = bytes - at;                             // bytes of the row from here on, 1 at least
         const uintptr_t p = reinterpret_cast<uintptr_t>(src + r * pitch + at);
         const uint32_t shift = (uint32_t)(p & 3) * 8;
@@ -34,7 +40,7 @@ __global__ void pad_rows_kernel(const uint8_t *__restrict__ src, int64_t pitch, 
             if (keep <= 0) o[k] = 0;
             else if (keep < 4) o[k] &= (1u << (8 * keep)) - 1u;
         }
-        dst[i] = make_uint4(o[0], o[1], o[2], o[3]);
+        dst[r * pieces + piece] = make_uint4(o[0], o[1], o[2], o[3]);
     }
 }
 
@@ -69,8 +75,12 @@ harp_status_t run(Call c, cudaStream_t s) {
     uint8_t *to = static_cast<uint8_t *>(scratch);
     for (const Operand &o : ops) {
         if (!o.bad(es)) continue;
-        const int64_t pieces = o.pieces(es), blocks = std::min<int64_t>((o.rows * pieces + 255) / 256, (int64_t)dev->sms * 16);
-        pad_rows_kernel<<<(unsigned)blocks, 256, 0, s>>>(static_cast<const uint8_t *>(*o.ptr), *o.ld * es, o.rows, o.d * es, reinterpret_cast<uint4 *>(to), pieces);
+        const bool weight = o.ptr == &c.other && c.product != GRAD_WEIGHTS;
+        // 64 pieces of four rows a CTA, and as many CTAs as are resident at once
+        const int64_t pieces = o.pieces(es), across = (pieces + 63) / 64;
+        const int64_t down = std::max<int64_t>(1, std::min<int64_t>((o.rows + 3) / 4, (int64_t)dev->sms * 8 / across));
+        pad_rows_kernel<<<dim3((unsigned)across, (unsigned)down), dim3(64, 4), 0, s>>>(static_cast<const uint8_t *>(*o.ptr), *o.ld * es, o.rows, o.d * es, reinterpret_cast<uint4 *>(to), pieces,
+                                                           weight ? c.offsets : nullptr, c.d_out);
         g_harp_launches.fetch_add(1, std::memory_order_relaxed);
         *o.ptr = to;
         *o.ld = pieces * 16 / es;
