@@ -410,14 +410,9 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             }
             const int blocks = to(T) - from(T);
             const bool any = blocks > 0;                     // ranks of a split may have none
-            float by_row[COLS / 64 ? COLS / 64 : 1];         // 8 bits: the rows' scales of this warp's chunks, a lane's column of each
-            if (I8 && (CG == 2 || P.split == 1)) {
-#pragma unroll
-                for (int i = 0; i < (int)(sizeof by_row / sizeof by_row[0]); ++i) {
-                    const int c = (2 * i + part) * 32 + lane;
-                    by_row[i] = c < T.cols ? P.row_scale[T.row0 + c] : 0.0f;
-                }
-            }
+            // 8 bits: the rows' scales of this warp's next chunk, one a lane
+            auto row_scale_of = [&](int c) { return I8 && c < T.cols ? P.row_scale[T.row0 + c] : 0.0f; };
+            float by_row = row_scale_of(part * 32 + lane);
             const int w = width(T);
             const bool whole = CG == 2 || P.split == 1;
             // the accumulator that is to be read next; and what it takes to hand it back
@@ -433,6 +428,7 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 if (lane == 0) mbar_arrive_at(CG == 2 ? map_rank(taken(n & 1), 0) : taken(n & 1));
                 ++n;
             };
+            constexpr int CHUNKS = COLS / 64 ? COLS / 64 : 1;        // of 32 columns, of this warp
             // this warp's columns: chunks of 32, or of 16 out of 32 where sums are divided among ranks
             float held[RUNS ? (COLS == 256 ? 128 : 32) : 1];
             if (RUNS) {
@@ -458,8 +454,9 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             const uint32_t d = accumulator();
             if (whole) {
                 const bool pairs = sizeof(Out) == 2 && P.pairs;
-#pragma unroll
-                for (int i = 0; i < (int)(sizeof by_row / sizeof by_row[0]); ++i) {
+                // (unrolled only where registers are indexed: four copies of the body missed the instruction cache, WITH_US)
+#pragma unroll (RUNS ? CHUNKS : 1)
+                for (int i = 0; i < CHUNKS; ++i) {
                     const int c0 = (2 * i + part) * 32;
                     if (c0 >= w) break;
                     uint32_t v[32];
@@ -469,9 +466,10 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                     } else tmem_ld32(d + c0, v);
                     if (I8) {
                         __syncwarp();
-                        s_scale[warp - 4][lane] = by_row[i];
+                        s_scale[warp - 4][lane] = by_row;
                         __syncwarp();
                     }
+                    if (I8) by_row = row_scale_of(c0 + 64 + lane);
                     if (!RUNS) tmem_wait_ld();
                     if (I8) {
                         const float4 *const scale = reinterpret_cast<const float4 *>(s_scale[warp - 4]);
@@ -689,7 +687,7 @@ Shape choose(const Call &c, const Device &dev) {
         for (int i = 0; i < 3; ++i) {
             const double n = (double)(met * tiles) * cols_of(cols), rounds = std::ceil(n / dev.clusters[i]);
             const double stretch = rounds > 1 ? 0.75 + 0.25 * rounds * dev.clusters[i] / n : 1;
-            const double join = i ? (cols == 32 ? 2.5 : 4) : 0.5;        // adding up a tile's sums
+            const double join = i ? (cols == 32 ? 2.5 : 6) : 0.5;        // adding up a tile's sums
             const double block = n * (1 << i) > dev.sms ? (cols == 32 ? 0.37 : 0.42) : (cols == 32 ? 0.285 : 0.36);
             const double t = std::max(memory * stretch, rounds * (blocks / (1 << i) * block + join)) + 3.5;
             if (t < least) {
