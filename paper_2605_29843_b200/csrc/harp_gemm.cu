@@ -89,6 +89,7 @@ __device__ __forceinline__ Tile tile_at(int t, const Params &P, const int *off, 
     if (PRODUCT == GRAD_WEIGHTS) {
         col_tiles = div_up(P.cols, P.tile_cols);
         tc = P.tile_cols;
+        // (a group at a time: with the groups in turn the stores go to all of them at once, fp32 gradients of 32 groups of 31 rows 189 -> 217 us)
         T.e = t / (lane_tiles * col_tiles);
         idx = t - T.e * (lane_tiles * col_tiles);
     } else {
@@ -454,7 +455,8 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             const uint32_t d = accumulator();
             if (whole) {
                 const bool pairs = sizeof(Out) == 2 && P.pairs;
-                // (unrolled only where registers are indexed: four copies of the body missed the instruction cache, WITH_US)
+                // (unrolled only where registers are indexed: four copies of the body missed the instruction cache: bf16 weight gradients of 32 groups
+                // of 31 rows, 2048 x 4096, 145 us, 118 this way)
 #pragma unroll (RUNS ? CHUNKS : 1)
                 for (int i = 0; i < CHUNKS; ++i) {
                     const int c0 = (2 * i + part) * 32;
@@ -671,8 +673,8 @@ Shape choose(const Call &c, const Device &dev) {
     const int64_t lanes = c.product == FORWARD ? c.d_out : c.d_in, pair_tiles = (lanes + 255) / 256, tiles = (lanes + 127) / 128;
     if (c.product == GRAD_WEIGHTS) return {256, 1, dev.pairs, c.n_groups * pair_tiles * ((c.d_out + 255) / 256)};
     const Shape pairs = {256, 1, dev.pairs, pair_tiles * ((c.n_rows + 255) / 256 + c.n_groups - 1)};
-    // rows of a group, and half as many again where there are several: they are not even
-    const int64_t met = std::min<int64_t>(c.n_groups, c.n_rows), even = (c.n_rows + met - 1) / met, rows = met > 1 ? even + even / 2 : even;
+    // rows of a group, and a quarter more where there are several: they are not even, but many fit a tile that the mean fits
+    const int64_t met = std::min<int64_t>(c.n_groups, c.n_rows), even = (c.n_rows + met - 1) / met, rows = met > 1 ? even + even / 4 : even;
     const double blocks = (double)(((c.product == FORWARD ? c.d_in : c.d_out) * (c.i8 ? 1 : 2) + 127) / 128), memory = (double)(met * tiles) * blocks * 16384 / 6.3e6;     // us
     auto cols_of = [&](int most) { return (double)((rows + most - 1) / most); };
     Shape best = pairs;
@@ -697,10 +699,6 @@ Shape choose(const Call &c, const Device &dev) {
         }
     return best;
 }
-
-}  // namespace
-
-namespace {
 
 bool describe(int dev, Device &d) {
     void *err = nullptr;
