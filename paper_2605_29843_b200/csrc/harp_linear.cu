@@ -9,6 +9,7 @@ namespace {
 using namespace harp_linear;
 
 constexpr int64_t kMostRows = 1ll << 30, kMostDim = 1ll << 20;
+constexpr int64_t kMostLd = 1ll << 37;           // the copy engine's rows lie less than 2^40 bytes apart
 constexpr int64_t kMostDepthI8 = 131071;         // 128 * 128 * d_in stays below 2^31
 
 bool aligned(const void *p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
@@ -53,7 +54,16 @@ struct Operand {
     int64_t pieces(int es) const { return (d * es + 15) / 16; }
 };
 
+// What a first call on a device asks for (attributes, a symbol's address, the pool) is no work of the stream: it may be asked for while
+// this thread captures.
+struct OutsideCapture {
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    OutsideCapture() { cudaThreadExchangeStreamCaptureMode(&mode); }
+    ~OutsideCapture() { cudaThreadExchangeStreamCaptureMode(&mode); }
+};
+
 harp_status_t run(Call c, cudaStream_t s) {
+    const OutsideCapture outside;
     const Device *dev = device();
     if (!dev) return HARP_ERR_UNSUPPORTED;
     const int es = c.i8 ? 1 : 2;
@@ -96,6 +106,10 @@ harp_status_t check_sizes(int64_t n_rows, int64_t d_in, int64_t d_out, int64_t n
     if (n_rows > kMostRows || d_in > kMostDim || d_out > kMostDim || n_groups > kMaxGroups) return HARP_ERR_TOO_LARGE;
     return HARP_OK;
 }
+harp_status_t check_ld(int64_t a, int64_t d_a, int64_t b, int64_t d_b, int64_t c, int64_t d_c) {
+    if (a < d_a || b < d_b || c < d_c) return HARP_ERR_BAD_DIM;
+    return a > kMostLd || b > kMostLd || c > kMostLd ? HARP_ERR_TOO_LARGE : HARP_OK;
+}
 harp_status_t check_out(const void *out, harp_dtype_t dtype) {
     return aligned(out, harp_dtype_size(dtype)) ? HARP_OK : HARP_ERR_BAD_DIM;
 }
@@ -107,7 +121,7 @@ harp_status_t linear_i8(const int8_t *x, int64_t ld_x, const float *x_scale, con
     harp_status_t st = check_sizes(n_rows, d_in, d_out, n_groups);
     if (st != HARP_OK) return st;
     if (d_in > kMostDepthI8) return HARP_ERR_TOO_LARGE;
-    if (ld_x < d_in || ld_w < d_in || ld_y < d_out) return HARP_ERR_BAD_DIM;
+    if ((st = check_ld(ld_x, d_in, ld_w, d_in, ld_y, d_out)) != HARP_OK) return st;
     if (n_rows == 0) return HARP_OK;
     if (!x || !x_scale || !w || !w_scale || !y || (grouped && !offsets)) return HARP_ERR_NULL;
     if (!aligned(x_scale, 4) || !aligned(w_scale, 4) || !aligned(offsets, 4)) return HARP_ERR_BAD_DIM;
@@ -143,7 +157,7 @@ harp_status_t harp_grouped_linear(const void *x, int64_t ld_x, const void *w, in
     if (y_dtype != HARP_F32 && y_dtype != HARP_BF16) return HARP_ERR_BAD_DTYPE;
     harp_status_t st = check_sizes(n_rows, d_in, d_out, n_groups);
     if (st != HARP_OK) return st;
-    if (ld_x < d_in || ld_w < d_in || ld_y < d_out) return HARP_ERR_BAD_DIM;
+    if ((st = check_ld(ld_x, d_in, ld_w, d_in, ld_y, d_out)) != HARP_OK) return st;
     if (n_rows == 0) return HARP_OK;
     if (!x || !w || !y || !offsets) return HARP_ERR_NULL;
     if (!aligned(x, 2) || !aligned(w, 2) || !aligned(offsets, 4)) return HARP_ERR_BAD_DIM;
@@ -163,7 +177,7 @@ harp_status_t harp_grouped_grad_rows(const void *gy, int64_t ld_gy, const void *
     if (gx_dtype != HARP_F32 && gx_dtype != HARP_BF16) return HARP_ERR_BAD_DTYPE;
     harp_status_t st = check_sizes(n_rows, d_in, d_out, n_groups);
     if (st != HARP_OK) return st;
-    if (ld_gy < d_out || ld_w < d_in || ld_gx < d_in) return HARP_ERR_BAD_DIM;
+    if ((st = check_ld(ld_gy, d_out, ld_w, d_in, ld_gx, d_in)) != HARP_OK) return st;
     if (n_rows == 0) return HARP_OK;
     if (!gy || !w || !gx || !offsets) return HARP_ERR_NULL;
     if (!aligned(gy, 2) || !aligned(w, 2) || !aligned(offsets, 4)) return HARP_ERR_BAD_DIM;
@@ -184,7 +198,7 @@ harp_status_t harp_grouped_grad_weights(const void *gy, int64_t ld_gy, const voi
     if (gw_dtype != HARP_F32 && gw_dtype != HARP_BF16) return HARP_ERR_BAD_DTYPE;
     harp_status_t st = check_sizes(n_rows, d_in, d_out, n_groups);
     if (st != HARP_OK) return st;
-    if (ld_gy < d_out || ld_x < d_in || ld_gw < d_in) return HARP_ERR_BAD_DIM;
+    if ((st = check_ld(ld_gy, d_out, ld_x, d_in, ld_gw, d_in)) != HARP_OK) return st;
     if (!gw || (n_rows > 0 && (!gy || !x || !offsets))) return HARP_ERR_NULL;
     if (!aligned(gy, 2) || !aligned(x, 2) || !aligned(offsets, 4)) return HARP_ERR_BAD_DIM;
     if ((st = check_out(gw, gw_dtype)) != HARP_OK) return st;

@@ -50,7 +50,8 @@ def grad_weights(gy=P, ld_gy=32, x=P, ld_x=64, off=P, groups=2, n=4, d_in=64, d_
     (linear, dict(ld_x=63), DIM), (linear, dict(ld_w=63), DIM), (linear, dict(ld_y=31), DIM), (linear, dict(y=P + 1), DIM),
     (linear, dict(y=P + 2, dtype=0), DIM), (linear, dict(xs=P + 1), DIM), (linear, dict(ws=P + 2), DIM),
     (linear, dict(d_in=131072, ld_x=131072, ld_w=131072), LARGE), (linear, dict(n=(1 << 30) + 1), LARGE),
-    (linear, dict(d_out=(1 << 20) + 1, ld_y=1 << 21), LARGE), (linear, dict(n=0, x=None, y=None), OK),
+    (linear, dict(d_out=(1 << 20) + 1, ld_y=1 << 21), LARGE), (linear, dict(ld_w=1 << 62), LARGE), (linear, dict(ld_y=1 << 38), LARGE),
+    (grad_rows, dict(ld_gy=1 << 38), LARGE), (grad_weights, dict(ld_gw=1 << 38), LARGE), (grouped, dict(ld_x=1 << 38), LARGE), (linear, dict(n=0, x=None, y=None), OK),
     *[(grouped_i8, {k: None}, NULL) for k in ("x", "xs", "w", "ws", "off", "y")],
     (grouped_i8, dict(groups=0), DIM), (grouped_i8, dict(groups=1025), LARGE), (grouped_i8, dict(off=P + 2), DIM),
     *[(grouped, {k: None}, NULL) for k in ("x", "w", "off", "y")],

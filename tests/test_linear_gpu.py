@@ -249,3 +249,38 @@ def test_grouped_grad_weights(sizes, d_in, d_out, accumulate, out):
             want = want + before[e].double()
             bound = bound + want.abs() * HALF[out] + before[e].double().abs() * 2.0 ** -23
         check(gw[e], want, bound)
+
+
+@pytest.mark.parametrize("d_in,d_out,ld_in,ld_out", [(200, 136, 256, 200), (201, 137, 208, 144), (64, 64, 72, 72), (203, 139, 203, 140), (77, 33, 81, 35)])
+@pytest.mark.parametrize("sizes", [[5, 0, 27], [300, 40]])
+def test_padding_leaves_no_trace(sizes, d_in, d_out, ld_in, ld_out):
+    """Rows longer than they say, NaN behind their ends, on the 16-byte grid and off it; what lies beside a result stays."""
+    n, off = sum(sizes), offsets_of(sizes)
+    x, gy = padded(normal(1, n, d_in).to(torch.bfloat16), ld_in), padded(normal(2, n, d_out).to(torch.bfloat16), ld_out)
+    w = padded(normal(3, len(sizes), d_out, d_in).to(torch.bfloat16), ld_in)
+    full = [torch.full((n, d_out + 3), -3.0, device="cuda"), torch.full((n, d_in + 5), -3.0, device="cuda"),
+            torch.full((len(sizes), d_out, d_in + 7), -3.0, device="cuda")]
+    y, gx, gw = full[0][:, :d_out], full[1][:, :d_in], full[2][..., :d_in]
+    harp.grouped_linear(x, w, off, out=y)
+    harp.grouped_grad_rows(gy, w, off, out=gx)
+    harp.grouped_grad_weights(gy, x, off, out=gw)
+    for e, r in group_rows(sizes):
+        check(y[r], *bf16_want(x[r], w[e], torch.float32))
+        check(gx[r], *bf16_want(gy[r], w[e].T, torch.float32))
+        check(gw[e], *bf16_want(gy[r].T, x[r].T, torch.float32))
+    assert (full[0][:, d_out:] == -3).all() and (full[1][:, d_in:] == -3).all() and (full[2][..., d_in:] == -3).all()
+
+
+@pytest.mark.parametrize("d", [9000, 20000])
+def test_long_fp32_sums(d):
+    """Sums of d products of one sign, which a tensor core's truncation would shrink by 1e-9 of the sum each: runs of 512 keep the error
+    below that of 512 additions cut off (2^-23 each) and d / 512 rounded ones."""
+    x, w = normal(1, 300, d).abs().to(torch.bfloat16), normal(2, 1, 256, d).abs().to(torch.bfloat16)
+    bound = 512 * 2.0 ** -23 / 16 + (d / 512 + 2) * 2.0 ** -24        # sixteen products an addition
+    for rows in (8, 300):
+        y = harp.grouped_linear(x[:rows], w, offsets_of([rows]), out_dtype=torch.float32).double()
+        want = x[:rows].double() @ w[0].double().T
+        assert ((y - want).abs() / want).max() <= bound
+    gw = harp.grouped_grad_weights(w[0].T.contiguous(), x.T.contiguous()[:, :296], offsets_of([d])).double()[0]
+    want = w[0].double() @ x[:296].double().T
+    assert ((gw - want).abs() / want).max() <= bound

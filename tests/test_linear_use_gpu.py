@@ -1,5 +1,9 @@
 """Layer products as a program uses them: in a chain, captured, on several streams, beside each other, at sizes past 32 bits, and
 what the torch conveniences refuse.  Bounds as in test_linear_gpu."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -196,6 +200,24 @@ def test_captured_and_replayed(misaligned):
     for k in OUTPUTS:
         assert torch.equal(s[k], t[k]), k
     assert harp.harp_linear_error_word() == 0
+
+
+@pytest.mark.parametrize("d_in", [512, 500])
+def test_the_first_call_of_a_process_may_be_captured(d_in):
+    code = f"""
+import torch
+import paper_2605_29843_b200 as harp
+x, w = torch.randn(37, {d_in}, device='cuda').bfloat16(), torch.randn(1, 64, {d_in}, device='cuda').bfloat16()
+off, y = torch.tensor([0, 37], dtype=torch.int32, device='cuda'), torch.zeros(37, 64, dtype=torch.bfloat16, device='cuda')
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    harp.grouped_linear(x, w, off, out=y)
+g.replay()
+torch.cuda.synchronize()
+z = harp.grouped_linear(x, w, off)
+assert torch.equal(y, z) and z.abs().sum() > 0
+"""
+    subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), check=True, timeout=100)
 
 
 @pytest.mark.parametrize("misaligned", [False, True])
