@@ -521,11 +521,10 @@ def two_sided_(w, plan_out: Plan, plan_in: Plan, scratch=None):
 # The products take matrices whose rows are contiguous (any row stride) on the current device, and write into `out` where it is
 # given.  What does not fit raises TypeError (dtypes) or ValueError (shapes, strides, devices) before the library is called.
 
-def _matrix(name, t, dtypes, dim, device):
-    """Leading dimension of a tensor of rows; a weight of several groups has them one behind the other."""
+def _matrix(name, t, shape, dtypes, dim, device):
+    """Leading dimension of a tensor of rows (of this shape, which its caller has); a weight of several groups has them one behind the other."""
     if t.dtype not in dtypes:
         raise TypeError(f"{name}: unsupported dtype {t.dtype}")
-    shape = t.shape
     if len(shape) != dim or t.get_device() != device:
         raise ValueError(f"{name}: {dim} dimensions on the current device expected, got {tuple(shape)} on {t.device}")
     if t.is_contiguous():
@@ -550,9 +549,10 @@ def _output(out, shape, dtype, like, device):
         return torch.empty(shape, dtype=dtype or torch.bfloat16, device=like.device), shape[-1]
     if dtype is not None and out.dtype is not dtype:
         raise TypeError(f"out: {dtype} expected, got {out.dtype}")
-    if out.shape != shape:
-        raise ValueError(f"out: shape {tuple(shape)} expected, got {tuple(out.shape)}")
-    return out, _matrix("out", out, _dtype_codes, len(shape), device)
+    got = out.shape
+    if got != shape:
+        raise ValueError(f"out: shape {tuple(shape)} expected, got {tuple(got)}")
+    return out, _matrix("out", out, got, _dtype_codes, len(shape), device)
 
 
 def quantize_rows(x, out=None, scale=None):
@@ -560,14 +560,16 @@ def quantize_rows(x, out=None, scale=None):
     if _apply_ex is None:
         _bind_torch()
     device = _current_device()
-    ld_x = _matrix("x", x, _dtype_codes, 2, device)
-    n, d = x.shape
+    shape = x.shape
+    ld_x = _matrix("x", x, shape, _dtype_codes, 2, device)
+    n, d = shape
     if out is None:
         out, ld_q = _output(None, (n, d), _i8[0], x, device)
     else:
-        ld_q = _matrix("out", out, _i8, 2, device)
-        if out.shape != x.shape:
-            raise ValueError(f"out: shape {tuple(x.shape)} expected, got {tuple(out.shape)}")
+        got = out.shape
+        ld_q = _matrix("out", out, got, _i8, 2, device)
+        if got != shape:
+            raise ValueError(f"out: shape {tuple(shape)} expected, got {tuple(got)}")
     if scale is None:
         scale = _output(None, (n,), _f32, x, device)[0]
     else:
@@ -583,8 +585,9 @@ def linear_i8(x, x_scale, w, w_scale, out=None, out_dtype=None):
     if _apply_ex is None:
         _bind_torch()
     device = _current_device()
-    ld_x, ld_w = _matrix("x", x, _i8, 2, device), _matrix("w", w, _i8, 2, device)
-    (n, d_in), (d_out, d_w) = x.shape, w.shape
+    x_shape, w_shape = x.shape, w.shape
+    ld_x, ld_w = _matrix("x", x, x_shape, _i8, 2, device), _matrix("w", w, w_shape, _i8, 2, device)
+    (n, d_in), (d_out, d_w) = x_shape, w_shape
     if d_w != d_in:
         raise ValueError(f"x has rows of {d_in} and w of {d_w}")
     _vector("x_scale", x_scale, _f32, n, device)
@@ -602,8 +605,9 @@ def grouped_linear_i8(x, x_scale, w, w_scale, offsets, out=None, out_dtype=None)
     if _apply_ex is None:
         _bind_torch()
     device = _current_device()
-    ld_x, ld_w = _matrix("x", x, _i8, 2, device), _matrix("w", w, _i8, 3, device)
-    (n, d_in), (groups, d_out, d_w) = x.shape, w.shape
+    x_shape, w_shape = x.shape, w.shape
+    ld_x, ld_w = _matrix("x", x, x_shape, _i8, 2, device), _matrix("w", w, w_shape, _i8, 3, device)
+    (n, d_in), (groups, d_out, d_w) = x_shape, w_shape
     if d_w != d_in:
         raise ValueError(f"x has rows of {d_in} and w of {d_w}")
     _vector("x_scale", x_scale, _f32, n, device)
@@ -623,8 +627,9 @@ def grouped_linear(x, w, offsets, out=None, out_dtype=None):
     if _apply_ex is None:
         _bind_torch()
     device = _current_device()
-    ld_x, ld_w = _matrix("x", x, _bf16, 2, device), _matrix("w", w, _bf16, 3, device)
-    (n, d_in), (groups, d_out, d_w) = x.shape, w.shape
+    x_shape, w_shape = x.shape, w.shape
+    ld_x, ld_w = _matrix("x", x, x_shape, _bf16, 2, device), _matrix("w", w, w_shape, _bf16, 3, device)
+    (n, d_in), (groups, d_out, d_w) = x_shape, w_shape
     if d_w != d_in:
         raise ValueError(f"x has rows of {d_in} and w of {d_w}")
     _vector("offsets", offsets, _i32, groups + 1, device)
@@ -641,8 +646,9 @@ def grouped_grad_rows(gy, w, offsets, out=None, out_dtype=None):
     if _apply_ex is None:
         _bind_torch()
     device = _current_device()
-    ld_gy, ld_w = _matrix("gy", gy, _bf16, 2, device), _matrix("w", w, _bf16, 3, device)
-    (n, d_gy), (groups, d_out, d_in) = gy.shape, w.shape
+    gy_shape, w_shape = gy.shape, w.shape
+    ld_gy, ld_w = _matrix("gy", gy, gy_shape, _bf16, 2, device), _matrix("w", w, w_shape, _bf16, 3, device)
+    (n, d_gy), (groups, d_out, d_in) = gy_shape, w_shape
     if d_gy != d_out:
         raise ValueError(f"gy has rows of {d_gy} and w {d_out} rows")
     _vector("offsets", offsets, _i32, groups + 1, device)
@@ -660,8 +666,9 @@ def grouped_grad_weights(gy, x, offsets, out=None, out_dtype=None, accumulate=Fa
     if _apply_ex is None:
         _bind_torch()
     device = _current_device()
-    ld_gy, ld_x = _matrix("gy", gy, _bf16, 2, device), _matrix("x", x, _bf16, 2, device)
-    (n, d_out), (n_x, d_in), groups = gy.shape, x.shape, offsets.numel() - 1
+    gy_shape, x_shape = gy.shape, x.shape
+    ld_gy, ld_x = _matrix("gy", gy, gy_shape, _bf16, 2, device), _matrix("x", x, x_shape, _bf16, 2, device)
+    (n, d_out), (n_x, d_in), groups = gy_shape, x_shape, offsets.numel() - 1
     if n != n_x:
         raise ValueError(f"gy has {n} rows and x {n_x}")
     if accumulate and out is None:
@@ -681,8 +688,8 @@ def processed_linear_i8(x, plan_in: Plan, plan_out: Plan, w, w_scale, out=None, 
     if _apply_ex is None:
         _bind_torch()
     device = _current_device()
-    _matrix("x", x, _dtype_codes, 2, device)
-    ld_w = _matrix("w", w, _i8, 2, device)
+    _matrix("x", x, x.shape, _dtype_codes, 2, device)
+    ld_w = _matrix("w", w, w.shape, _i8, 2, device)
     n = x.shape[0]
     if not x.is_contiguous() or x.shape[1] != plan_in.d or w.shape != (plan_out.d, plan_in.d):
         raise ValueError(f"contiguous rows of {plan_in.d} and a weight {(plan_out.d, plan_in.d)} expected, got {tuple(x.shape)} and {tuple(w.shape)}")

@@ -50,9 +50,10 @@ constexpr int kHalf = 16384;                 // the lane operand's part of a sta
 // rounding to nearest: 5e-7 at any length.  bf16 results round off 2^-9 in any case and take one run.
 constexpr int kRun = 8;                      // blocks
 constexpr int kSumCols = 32;                 // columns whose sums a split adds up at a time
-// COLS: most columns of a tile (256 for a pair of CTAs, 32 or 64 for one)
+// COLS: most columns of a tile (256 for a pair of CTAs, 32 or 64 for one).  DEEP: a single CTA has the SM for itself, and the shared memory;
+// else it leaves room for another one
 __host__ __device__ constexpr int stage_bytes(int cols) { return kHalf + (cols == 256 ? 128 : cols) * 128; }
-__host__ __device__ constexpr int stages(int cols) { return cols == 256 ? 6 : cols == 64 ? 3 : 4; }      // one CTA leaves room for another one
+__host__ __device__ constexpr int stages(int cols, bool deep) { return cols == 256 ? 6 : cols == 64 ? (deep ? 7 : 3) : deep ? 9 : 4; }
 constexpr uint32_t kSpin = 1u << 22;         // limit of every wait
 constexpr int kMostSmem = 232448 - 4096;     // dynamic shared memory, less what the kernels have besides
 
@@ -177,13 +178,13 @@ __device__ __forceinline__ uint32_t pack_bf16(uint32_t lo, uint32_t hi) {
     return r;
 }
 
-template <bool I8, int COLS, int PRODUCT, typename Out>
-__global__ void __launch_bounds__(kThreads, COLS == 256 ? 1 : 2)
+template <bool I8, int COLS, bool DEEP, int PRODUCT, typename Out>
+__global__ void __launch_bounds__(kThreads, COLS == 256 || DEEP ? 1 : 2)
 harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                  const __grid_constant__ CUtensorMap map_b_small, const Params P) {
     constexpr int BLOCK = I8 ? 128 : 64;                     // contracted elements a stage
     constexpr int CG = COLS == 256 ? 2 : 1;                  // CTAs a tile
-    constexpr int STAGES = stages(COLS), kStage = stage_bytes(COLS);
+    constexpr int STAGES = stages(COLS, DEEP), kStage = stage_bytes(COLS);
     constexpr bool A_MN = PRODUCT != FORWARD, B_MN = PRODUCT == GRAD_WEIGHTS;
     constexpr bool RUNS = !I8 && sizeof(Out) == 4;           // sums of runs of blocks are added up in registers
     constexpr int RUN = RUNS ? kRun : 1 << 30;
@@ -621,19 +622,19 @@ bool encode(CUtensorMap *map, bool i8, const void *ptr, int rank, const int64_t 
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-int smem_bytes(int cols, int split, int n_groups) {
-    return 1024 + stages(cols) * stage_bytes(cols) + (split > 1 ? kSumCols * 512 : 0) + 8 * (n_groups + 1);
+int smem_bytes(int cols, bool deep, int split, int n_groups) {
+    return 1024 + stages(cols, deep) * stage_bytes(cols) + (split > 1 ? kSumCols * 512 : 0) + 8 * (n_groups + 1);
 }
 
-template <bool I8, int COLS, int PRODUCT, typename Out>
+template <bool I8, int COLS, bool DEEP, int PRODUCT, typename Out>
 harp_status_t launch(const CUtensorMap (&maps)[3], const Params &P, int clusters, cudaStream_t s) {
-    const auto kernel = harp_gemm_kernel<I8, COLS, PRODUCT, Out>;
+    const auto kernel = harp_gemm_kernel<I8, COLS, DEEP, PRODUCT, Out>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem) != cudaSuccess) return HARP_ERR_CUDA;
     const int size = COLS == 256 ? 2 : P.split;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(clusters * size));
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = (size_t)smem_bytes(COLS, P.split, P.n_groups);
+    cfg.dynamicSmemBytes = (size_t)smem_bytes(COLS, DEEP, P.split, P.n_groups);
     cfg.stream = s;
     cudaLaunchAttribute la[2];
     la[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -652,9 +653,9 @@ harp_status_t launch(const CUtensorMap (&maps)[3], const Params &P, int clusters
     return HARP_OK;
 }
 
-template <bool I8, int COLS, int PRODUCT>
+template <bool I8, int COLS, bool DEEP, int PRODUCT>
 harp_status_t launch(harp_dtype_t out, const CUtensorMap (&maps)[3], const Params &P, int clusters, cudaStream_t s) {
-    return out == HARP_F32 ? launch<I8, COLS, PRODUCT, float>(maps, P, clusters, s) : launch<I8, COLS, PRODUCT, __nv_bfloat16>(maps, P, clusters, s);
+    return out == HARP_F32 ? launch<I8, COLS, DEEP, PRODUCT, float>(maps, P, clusters, s) : launch<I8, COLS, DEEP, PRODUCT, __nv_bfloat16>(maps, P, clusters, s);
 }
 
 // How a call is cut: by pairs of CTAs on 256 lanes x 256 columns, or by single ones on 128 x 32 or 128 x 64 in clusters of `split`.
@@ -697,7 +698,7 @@ Shape choose(const Call &c, const Device &dev) {
             const double stretch = rounds > 1 ? 0.75 + 0.25 * rounds * dev.clusters[i] / n : 1;
             const double join = i ? (cols == 32 ? 2.5 : 6) : 0.5;        // adding up a tile's sums
             const double block = n * (1 << i) > dev.sms ? (cols == 32 ? 0.37 : 0.42) : (cols == 32 ? 0.285 : 0.36);
-            const double t = std::max(memory * stretch, rounds * (blocks / (1 << i) * block + join)) + 3.5;
+            const double t = std::max(memory * stretch + join, rounds * (blocks / (1 << i) * block + join)) + 3.5;
             if (t < least) {
                 least = t;
                 best = {cols, 1 << i, dev.clusters[i], tiles * ((c.n_rows + cols - 1) / cols + c.n_groups - 1)};
@@ -715,7 +716,7 @@ bool describe(int dev, Device &d) {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3((unsigned)(d.sms / size * size));
         cfg.blockDim = dim3(kThreads);
-        cfg.dynamicSmemBytes = (size_t)smem_bytes(cols, cols == 256 ? 1 : size, kMaxGroups);
+        cfg.dynamicSmemBytes = (size_t)smem_bytes(cols, false, cols == 256 ? 1 : size, kMaxGroups);
         cudaLaunchAttribute la;
         la.id = cudaLaunchAttributeClusterDimension;
         la.val.clusterDim.x = (unsigned)size;
@@ -727,9 +728,9 @@ bool describe(int dev, Device &d) {
                         cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess;
         return ok ? n : 0;
     };
-    d.pairs = resident(harp_gemm_kernel<false, 256, FORWARD, __nv_bfloat16>, 256, 2);
+    d.pairs = resident(harp_gemm_kernel<false, 256, false, FORWARD, __nv_bfloat16>, 256, 2);
     // (the query counts one CTA an SM wherever tensor memory is used; two of these fit, and run)
-    for (int i = 0; i < 3; ++i) d.clusters[i] = 2 * resident(harp_gemm_kernel<false, 32, FORWARD, __nv_bfloat16>, 32, 1 << i);
+    for (int i = 0; i < 3; ++i) d.clusters[i] = 2 * resident(harp_gemm_kernel<false, 32, false, FORWARD, __nv_bfloat16>, 32, 1 << i);
     d.err = static_cast<int32_t *>(err);
     return d.pairs > 0 && d.clusters[0] > 0 && d.clusters[1] > 0 && d.clusters[2] > 0;
 }
@@ -814,14 +815,18 @@ harp_status_t gemm(const Call &c, const Device &dev, cudaStream_t stream) {
         ok = ok && encode(&maps[1], c.i8, c.rows, 2, e, p, box) && encode(&maps[2], c.i8, c.rows, 2, e, p, box_small);
     }
     if (!ok) return HARP_ERR_UNSUPPORTED;
+    // All tiles at once and one CTA an SM at most: a longer ring (1 row, 4096 -> 14336 14.9 -> 14.0 us, 64 rows 17.7 -> 15.3 us; clusters on
+    // 32 columns are better off with the next kernel's CTAs beside them, 1 row 4096 -> 4096 8.0 against 8.5 us).
+    const bool deep = shape.tiles * shape.split <= dev.sms && shape.tiles <= shape.slots / 2 && (shape.split == 1 || shape.cols == 64);
     auto by_cols = [&](auto i8, auto product) {
         constexpr bool I8 = decltype(i8)::value;
         constexpr int PRODUCT = decltype(product)::value;
-        if (shape.cols == 32) return launch<I8, 32, PRODUCT>(c.out_dtype, maps, P, clusters, stream);
-        if (shape.cols == 64) return launch<I8, 64, PRODUCT>(c.out_dtype, maps, P, clusters, stream);
-        return launch<I8, 256, PRODUCT>(c.out_dtype, maps, P, clusters, stream);
+        if (shape.cols == 256) return launch<I8, 256, false, PRODUCT>(c.out_dtype, maps, P, clusters, stream);
+        if (shape.cols == 64)
+            return deep ? launch<I8, 64, true, PRODUCT>(c.out_dtype, maps, P, clusters, stream) : launch<I8, 64, false, PRODUCT>(c.out_dtype, maps, P, clusters, stream);
+        return deep ? launch<I8, 32, true, PRODUCT>(c.out_dtype, maps, P, clusters, stream) : launch<I8, 32, false, PRODUCT>(c.out_dtype, maps, P, clusters, stream);
     };
-    if (c.product == GRAD_WEIGHTS) return launch<false, 256, GRAD_WEIGHTS>(c.out_dtype, maps, P, clusters, stream);
+    if (c.product == GRAD_WEIGHTS) return launch<false, 256, false, GRAD_WEIGHTS>(c.out_dtype, maps, P, clusters, stream);
     if (c.product == GRAD_ROWS) return by_cols(std::false_type(), std::integral_constant<int, GRAD_ROWS>());
     return c.i8 ? by_cols(std::true_type(), std::integral_constant<int, FORWARD>()) : by_cols(std::false_type(), std::integral_constant<int, FORWARD>());
 }
