@@ -87,48 +87,65 @@ __device__ __forceinline__ int even_cols(int n, int most) {
     return n <= 0 ? most : round_up(div_up(n, div_up(n, most)), CG == 2 ? 32 : 16);
 }
 
-// Which tile is number t.  Neighbouring numbers share operands: bands of eight lane tiles, column tiles along a band.
+// Which tile is number t, for rising t.  Neighbouring numbers share operands: bands of eight lane tiles, column tiles along a band.  Every
+// role walks over the tiles by itself, from the group and band of its last one on: finding them by division took longer than the rest of
+// a short tile (COMPARE_US).
 template <int CG, int PRODUCT, int BLOCK>
-__device__ __forceinline__ Tile tile_at(int t, const Params &P, const int *off, const int *first) {
-    Tile T;
-    const int lane_tiles = div_up(P.lanes, 128 * CG);
-    int idx, col_tiles, tc;
-    if (PRODUCT == GRAD_WEIGHTS) {
-        col_tiles = div_up(P.cols, P.tile_cols);
-        tc = P.tile_cols;
-        // (a group at a time: with the groups in turn the stores go to all of them at once, fp32 gradients of 32 groups of 31 rows 189 -> 217 us)
-        T.e = t / (lane_tiles * col_tiles);
-        idx = t - T.e * (lane_tiles * col_tiles);
-    } else {
-        int lo = 0, hi = P.n_groups;             // the last group whose first tile is at or below t
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (first[mid] <= t) lo = mid;
-            else hi = mid;
+struct Walk {
+    const Params &P;
+    const int *off, *first;
+    int lane_tiles, e, start, rows, tile_cols, col_tiles, band, band_start;      // start: number of the group's first tile; band_start: from there on
+
+    __device__ __forceinline__ Walk(const Params &P_, const int *off_, const int *first_) : P(P_), off(off_), first(first_) {
+        lane_tiles = div_up(P.lanes, 128 * CG);
+        start = 0;
+        if (PRODUCT == GRAD_WEIGHTS) {
+            tile_cols = P.tile_cols;
+            col_tiles = div_up(P.cols, P.tile_cols);
         }
-        T.e = lo;
-        idx = t - first[lo];
-        tc = even_cols<CG>(off[lo + 1] - off[lo], P.tile_cols);
-        col_tiles = div_up(off[lo + 1] - off[lo], tc);
+        enter(0);
     }
-    const int band = idx / (8 * col_tiles), in_band = idx - band * 8 * col_tiles;
-    const int width = min(8, lane_tiles - band * 8);
-    T.lane0 = (band * 8 + in_band % width) * 128 * CG;
-    T.col0 = (in_band / width) * tc;
-    const int n = off[T.e + 1] - off[T.e];
-    if (PRODUCT == GRAD_WEIGHTS) {
-        T.cols = min(tc, P.cols - T.col0);
-        T.row0 = off[T.e];
-        T.blocks = div_up(n, BLOCK);
-        T.tail = n - (T.blocks - 1) * BLOCK;
-    } else {
-        T.cols = min(tc, n - T.col0);
-        T.row0 = off[T.e] + T.col0;
-        T.blocks = div_up(P.depth, BLOCK);
-        T.tail = BLOCK;
+    __device__ __forceinline__ void enter(int group) {
+        e = group;
+        band = band_start = 0;
+        rows = off[e + 1] - off[e];
+        if (PRODUCT != GRAD_WEIGHTS) {
+            start = first[e];
+            tile_cols = even_cols<CG>(rows, P.tile_cols);
+            col_tiles = div_up(rows, tile_cols);
+        }
     }
-    return T;
-}
+    __device__ __forceinline__ Tile at(int t) {
+        if (PRODUCT == GRAD_WEIGHTS) {
+            int group = e;
+            while (t - start >= lane_tiles * col_tiles) start += lane_tiles * col_tiles, ++group;
+            if (group != e) enter(group);
+        } else {
+            int group = e;
+            while (first[group + 1] <= t) ++group;
+            if (group != e) enter(group);
+        }
+        while (t - start - band_start >= 8 * col_tiles) band_start += 8 * col_tiles, ++band;
+        const int in_band = t - start - band_start, width = min(8, lane_tiles - band * 8);
+        const int col = width == 8 ? in_band >> 3 : in_band / width;
+        Tile T;
+        T.e = e;
+        T.lane0 = (band * 8 + in_band - col * width) * 128 * CG;
+        T.col0 = col * tile_cols;
+        if (PRODUCT == GRAD_WEIGHTS) {
+            T.cols = min(tile_cols, P.cols - T.col0);
+            T.row0 = off[e];
+            T.blocks = div_up(rows, BLOCK);
+            T.tail = rows - (T.blocks - 1) * BLOCK;
+        } else {
+            T.cols = min(tile_cols, rows - T.col0);
+            T.row0 = off[e] + T.col0;
+            T.blocks = div_up(P.depth, BLOCK);
+            T.tail = BLOCK;
+        }
+        return T;
+    }
+};
 
 struct Waiter {
     volatile int *dead;
@@ -282,7 +299,7 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     const uint32_t columns = s_columns;
     const Waiter wait{&s_dead, P.err};
     const int n_tiles = PRODUCT == GRAD_WEIGHTS ? P.n_groups * div_up(P.lanes, 128 * CG) * div_up(P.cols, P.tile_cols) : first[P.n_groups];
-    auto at = [&](int t) { return tile_at<CG, PRODUCT, BLOCK>(t, P, off, first); };
+    using Tiles = Walk<CG, PRODUCT, BLOCK>;
     // this CTA's share of the blocks
     auto from = [&](const Tile &T) { return CG == 2 ? 0 : (int)((int64_t)T.blocks * (int)rank / P.split); };
     auto to = [&](const Tile &T) { return CG == 2 ? T.blocks : (int)((int64_t)T.blocks * ((int)rank + 1) / P.split); };
@@ -290,11 +307,12 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     auto is_ragged = [&](const Tile &T, int b) { return PRODUCT == GRAD_WEIGHTS && b == T.blocks - 1 && T.tail % 16 != 0; };
 
     if (warp == 0 && lane == 0) {
+        Tiles tiles(P, off, first);
         Ring<STAGES> ring;
         uint32_t used = 0;                                   // a bit for each stage that a copy went to
         bool alive = true;
         for (int t = cluster; alive && t < n_tiles; t += clusters) {
-            const Tile T = at(t);
+            const Tile T = tiles.at(t);
             const int half = width(T) / CG;                  // columns of this CTA
             const int lane0 = T.lane0 + (CG == 2 ? (int)rank * 128 : 0), col0 = CG == 2 ? (int)rank * half : 0;
             // rows along the columns: one copy of 128 of them, or copies of 32
@@ -337,11 +355,12 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 for (uint32_t i = 0; (used >> s & 1) && i < kSpin && !mbar_try(full(s), s < ring.s ? ring.phase : ring.phase ^ 1); ++i) {}
         }
     } else if (warp == 1 && lane == 0 && (CG == 1 || rank == 0)) {
+        Tiles tiles(P, off, first);
         Ring<STAGES> ring;
         int n = 0;
         bool alive = true;
         for (int t = cluster; alive && t < n_tiles; t += clusters) {
-            const Tile T = at(t);
+            const Tile T = tiles.at(t);
             const int b1 = to(T);
             const uint32_t idesc = instr(I8, A_MN, B_MN, 128 * CG, width(T));
             for (int b = from(T); alive && b < b1; ++n) {
@@ -370,10 +389,11 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         }
     } else if (warp == 2 && PRODUCT == GRAD_WEIGHTS) {
         // the other groups' rows of a ragged last block
+        Tiles tiles(P, off, first);
         Ring<STAGES> ring;
         uint32_t phases = 0;                                 // a bit a stage: its next ragged block's phase
         for (int t = cluster; t < n_tiles; t += clusters) {
-            const Tile T = at(t);
+            const Tile T = tiles.at(t);
             if (T.blocks == 0) continue;
             ring.skip(T.blocks - 1);
             if (is_ragged(T, T.blocks - 1)) {
@@ -401,11 +421,12 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         }
     } else if (warp >= 4) {
         const int q = warp & 3, part = (warp - 4) >> 2;      // lanes 32 q .. 32 q + 31; chunks of 32 columns alternate between the two warps
+        Tiles tiles(P, off, first);
         int n = 0;
         uint32_t sums_phase = 0;
         bool alive = true;
         for (int t = cluster; t < n_tiles; t += clusters) {
-            const Tile T = at(t);
+            const Tile T = tiles.at(t);
             const int l = T.lane0 + (CG == 2 ? (int)rank * 128 : 0) + q * 32 + lane;
             const bool inside = l < P.lanes;
             Out *const out = static_cast<Out *>(P.out) +
