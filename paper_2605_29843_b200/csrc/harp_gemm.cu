@@ -49,6 +49,7 @@ constexpr int kHalf = 16384;                 // the lane operand's part of a sta
 // 1.1e-9 of itself a product (1.6e-5 after 14336).  Results in fp32 are therefore summed in runs of 512 products, which the epilogue adds up,
 // rounding to nearest: 5e-7 at any length.  bf16 results round off 2^-9 in any case and take one run.
 constexpr int kRun = 8;                      // blocks
+constexpr int kTurnBytes = 8 * 2048;         // where the epilogue warps of a pair's CTA turn bf16 results round
 constexpr int kSumCols = 32;                 // columns whose sums a split adds up at a time
 // COLS: most columns of a tile (256 for a pair of CTAs, 32 or 64 for one).  DEEP: a single CTA has the SM for itself, and the shared memory;
 // else it leaves room for another one
@@ -70,7 +71,7 @@ struct Params {
     const float *row_scale, *channel_scale;
     int32_t accumulate;
     int32_t chunked_a, chunked_b;            // MN-major operands: both chunks of 64 by one copy
-    int32_t pairs;                           // bf16 results may be stored two lanes at a time
+    int32_t pairs, eights;                   // bf16 results may be stored two, eight lanes at a time
     int32_t *err;
 };
 
@@ -220,7 +221,7 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     unsigned char *const base_ptr = smem_raw + (base - smem_u32(smem_raw));
     const uint32_t sums = base + STAGES * kStage;            // the other ranks' accumulators (split > 1)
-    int *const off = reinterpret_cast<int *>(base_ptr + STAGES * kStage + (CG == 1 && P.split > 1 ? kSumCols * 512 : 0));
+    int *const off = reinterpret_cast<int *>(base_ptr + STAGES * kStage + (CG == 2 ? kTurnBytes : P.split > 1 ? kSumCols * 512 : 0));
     int *const first = off + P.n_groups + 1;
 
     const uint32_t bar0 = smem_u32(bars);
@@ -481,7 +482,60 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 if (!alive) break;
             } else if (any && !arrived()) break;
             const uint32_t d = accumulator();
-            if (whole) {
+            if (CG == 2 && sizeof(Out) == 2 && P.eights) {
+                // Results as mma.sync's fragments, pairs of columns packed, turned round in shared memory: eight lanes of a column are 16 bytes there.
+                // A third of the instructions that storing lane by lane takes (COMPARE).
+                unsigned char *const turn = base_ptr + STAGES * kStage + (warp - 4) * 2048;      // 32 columns of 64 bytes
+                const uint32_t turn_s = smem_u32(turn);
+                auto place = [](int c, int eight) { return c * 64 + ((eight ^ (c >> 1 & 3)) << 4); };
+                float by_lanes[4];                           // 8 bits: scales of lanes lane / 4 + 8 h
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    const int ch = T.lane0 + (int)rank * 128 + q * 32 + h * 8 + (lane >> 2);
+                    by_lanes[h] = I8 && ch < P.lanes ? P.channel_scale[(int64_t)T.e * P.lanes + ch] : 0.0f;
+                }
+                const bool eight_inside = T.lane0 + (int)rank * 128 + q * 32 + (lane & 3) * 8 < P.lanes;
+                Out *const to = out - lane + (lane & 3) * 8 + (int64_t)(lane >> 2) * P.ld_out;
+#pragma unroll 1
+                for (int c0 = part * 32; c0 < w; c0 += 64) {
+                    uint32_t v[2][16];
+                    load_fragments(d + c0, v[0]);
+                    load_fragments(d + (16u << 16) + c0, v[1]);
+                    __syncwarp();                            // what was turned round before has been read
+                    if (I8) s_scale[warp - 4][lane] = by_row;
+                    if (I8) __syncwarp();
+                    if (I8) by_row = row_scale_of(c0 + 64 + lane);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int j = 0; j < 4; j += 2) {
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {        // lanes 16 k .. 16 k + 15
+                            uint32_t tiles[4];
+#pragma unroll
+                            for (int m = 0; m < 4; ++m) {    // eight columns, eight lanes
+                                const int jj = j + m / 2, h = m & 1;
+                                uint32_t lo = v[k][4 * jj + 2 * h], hi = v[k][4 * jj + 2 * h + 1];
+                                if (I8) {
+                                    const float2 r = *reinterpret_cast<const float2 *>(&s_scale[warp - 4][8 * jj + 2 * (lane & 3)]);
+                                    lo = __float_as_uint((float)(int32_t)lo * by_lanes[2 * k + h] * r.x);
+                                    hi = __float_as_uint((float)(int32_t)hi * by_lanes[2 * k + h] * r.y);
+                                }
+                                tiles[m] = pack_bf16(lo, hi);
+                            }
+                            const int c = 8 * (j + (lane >> 4)) + (lane & 7);
+                            store_transposed(turn_s + place(c, 2 * k + (lane >> 3 & 1)), tiles[0], tiles[1], tiles[2], tiles[3]);
+                        }
+                    }
+                    __syncwarp();
+                    Out *p = to + (int64_t)c0 * P.ld_out;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i, p += 8 * P.ld_out) {
+                        const int c = i * 8 + (lane >> 2);
+                        const uint4 eight = *reinterpret_cast<const uint4 *>(turn + place(c, lane & 3));
+                        if (eight_inside && c0 + c < T.cols) *reinterpret_cast<uint4 *>(p) = eight;
+                    }
+                }
+            } else if (whole) {
                 const bool pairs = sizeof(Out) == 2 && P.pairs;
                 // (unrolled only where registers are indexed: four copies of the body missed the instruction cache: bf16 weight gradients of 32 groups
                 // of 31 rows, 2048 x 4096, 145 us, 118 this way)
@@ -644,7 +698,7 @@ bool encode(CUtensorMap *map, bool i8, const void *ptr, int rank, const int64_t 
 }
 
 int smem_bytes(int cols, bool deep, int split, int n_groups) {
-    return 1024 + stages(cols, deep) * stage_bytes(cols) + (split > 1 ? kSumCols * 512 : 0) + 8 * (n_groups + 1);
+    return 1024 + stages(cols, deep) * stage_bytes(cols) + (cols == 256 ? kTurnBytes : split > 1 ? kSumCols * 512 : 0) + 8 * (n_groups + 1);
 }
 
 template <bool I8, int COLS, bool DEEP, int PRODUCT, typename Out>
@@ -798,6 +852,7 @@ harp_status_t gemm(const Call &c, const Device &dev, cudaStream_t stream) {
     P.cols = (int32_t)c.d_out;
     P.depth = (int32_t)(c.product == FORWARD ? c.d_in : c.d_out);
     P.pairs = reinterpret_cast<uintptr_t>(c.out) % 4 == 0 && c.ld_out % 2 == 0 && P.lanes % 2 == 0 && !c.accumulate;
+    P.eights = P.pairs && reinterpret_cast<uintptr_t>(c.out) % 16 == 0 && c.ld_out % 8 == 0 && P.lanes % 8 == 0;
     const Shape shape = choose(c, dev);
     if (shape.tiles > INT32_MAX / 16) return HARP_ERR_TOO_LARGE;
     P.tile_cols = shape.cols;

@@ -110,6 +110,17 @@ __device__ __forceinline__ void commit(uint32_t bar) {
                      ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
 
+// 16 lanes x 32 columns of tensor memory as the fragments of mma.sync's accumulators: v[4 j + 2 h + i] of thread t is lane t / 4 + 8 h,
+// column 8 j + 2 (t % 4) + i
+__device__ __forceinline__ void load_fragments(uint32_t taddr, uint32_t (&v)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]) : "r"(taddr) : "memory");
+}
+// four 8 x 8 tiles of 16-bit values, transposed: lane t gives the address of row t % 8 of tile t / 8
+__device__ __forceinline__ void store_transposed(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
 // Operand descriptor, 128-byte swizzle.  K-major: rows of 128 bytes, eight rows a kilobyte (sbo).  MN-major: chunks of 64
 // elements along M or N `lbo` apart, eight steps along K a kilobyte (sbo).
 __device__ __forceinline__ uint64_t operand(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
