@@ -43,7 +43,7 @@ namespace {
 
 using namespace harp_gemm_ptx;
 
-constexpr int kThreads = 384;                // warps: 0 copies, 1 products, 2 tensor memory and ragged ends, 3 offsets, 4-11 epilogue (two a lane quarter)
+constexpr int kThreads = 384;                // warps: 0 copies, 1 products, 2 tensor memory, 3 offsets, then both ragged ends, 4-11 epilogue (two a lane quarter)
 constexpr int kHalf = 16384;                 // the lane operand's part of a stage in one CTA
 // The tensor core cuts its fp32 sums off instead of rounding them, sixteen products at a time: the result of a long sum is too small by
 // 1.1e-9 of itself a product (1.6e-5 after 14336).  Results in fp32 are therefore summed in runs of 512 products, which the epilogue adds up,
@@ -388,8 +388,10 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 if (alive) commit<CG>(done(acc));
             }
         }
-    } else if (warp == 2 && PRODUCT == GRAD_WEIGHTS) {
-        // the other groups' rows of a ragged last block
+    } else if ((warp == 2 || warp == 3) && PRODUCT == GRAD_WEIGHTS) {
+        // The other groups' rows of a ragged last block.  One takes some 2800 cycles (stores, the fence to the asynchronous side, the
+        // release to the other CTA), a short tile's stores 2500: two warps take one for even stages, one for odd ones (not blocks in turn:
+        // a warp that waits for a stage's phase after the next one finds the one before that, and goes on at once).
         Tiles tiles(P, off, first);
         Ring<STAGES> ring;
         uint32_t phases = 0;                                 // a bit a stage: its next ragged block's phase
@@ -398,6 +400,10 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             if (T.blocks == 0) continue;
             ring.skip(T.blocks - 1);
             if (is_ragged(T, T.blocks - 1)) {
+                if ((ring.s ^ warp) & 1) {
+                    ring.next();
+                    continue;
+                }
                 const uint32_t phase = phases >> ring.s & 1;
                 phases ^= 1u << ring.s;
                 if (!wait(ragged(ring.s), phase, 4)) break;

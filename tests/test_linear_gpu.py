@@ -175,7 +175,8 @@ def test_linear_i8_strides(rows, ldx, ldw, ldy, sx, sw):
 GROUPS = [
     ([1], 64, 64), ([5, 0, 3], 128, 96), ([0, 0, 7, 0], 256, 200), ([0], 64, 64), ([16, 16, 16, 16], 512, 512), ([1] * 40, 256, 320),
     ([17, 1, 33, 0, 63, 64, 65], 264, 136), ([300, 0, 5], 2048, 512), ([130, 129, 128, 127], 1001, 515), ([257, 255, 600], 512, 1000),
-    ([0, 1000, 0, 24], 4096, 264), ([3] * 129, 72, 72), ([2, 700, 31, 1], 40, 24), ([515], 1, 1), ([127, 1, 70, 15], 4096, 4096), ([40, 60], 1, 300), ([40, 60], 300, 1)]
+    ([0, 1000, 0, 24], 4096, 264), ([3] * 129, 72, 72), ([2, 700, 31, 1], 40, 24), ([515], 1, 1), ([127, 1, 70, 15], 4096, 4096),
+    ([751, 383, 10], 4096, 2048), ([40, 60], 1, 300), ([40, 60], 300, 1)]
 
 
 def group_rows(sizes, start=0):
