@@ -90,7 +90,7 @@ __device__ __forceinline__ int even_cols(int n, int most) {
 
 // Which tile is number t, for rising t.  Neighbouring numbers share operands: bands of eight lane tiles, column tiles along a band.  Every
 // role walks over the tiles by itself, from the group and band of its last one on: finding them by division took longer than the rest of
-// a short tile (COMPARE_US).
+// a short tile (bf16 weight gradients of 32 groups of 31 rows 118 -> 111 us).
 template <int CG, int PRODUCT, int BLOCK>
 struct Walk {
     const Params &P;
@@ -490,7 +490,7 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             const uint32_t d = accumulator();
             if (CG == 2 && sizeof(Out) == 2 && P.eights) {
                 // Results as mma.sync's fragments, pairs of columns packed, turned round in shared memory: eight lanes of a column are 16 bytes there.
-                // A third of the instructions that storing lane by lane takes (COMPARE).
+                // A third of the instructions that storing lane by lane takes (8 bits, 16384 x 4096 x 14336 655 -> 619 us).
                 unsigned char *const turn = base_ptr + STAGES * kStage + (warp - 4) * 2048;      // 32 columns of 64 bytes
                 const uint32_t turn_s = smem_u32(turn);
                 auto place = [](int c, int eight) { return c * 64 + ((eight ^ (c >> 1 & 3)) << 4); };
