@@ -15,11 +15,12 @@
 // accumulators through distributed shared memory, in the order of their ranks.  Tiles are handed out round robin; two
 // accumulators fit tensor memory, so a tile's epilogue runs under the next one's products.
 //
-// What bounds it (B200, 1965 MHz, 6538 GB/s and 1670 bf16 TFLOP/s measured).  Large products: the way from L2, which gives 9.8 TB/s to
-// 4096 rows over 8 groups, 8192 -> 4096 (tensor pipe 73 %), and under load the power limit: 8192^3 in 8 bits 342 us (3.2 POP/s; 366 in a long
-// run), in bf16 729 us (1.51 PFLOP/s, the library's product 677; 786 and 738 in a long run).  Few rows: the weight's bytes: 8 groups of 4 rows, 4096 ->
-// 14336, 147 us (6.4 TB/s); one row, 8192 -> 28672 in 8 bits, 42 us (5.6 TB/s); below some 60 MB the 4 to 5 us that a launch,
-// the first copy's way and the last stores take: 4096 -> 14336 15 us, 4096 -> 4096 8 us.  Weight gradients of short groups: their stores.
+// What bounds it (B200, 1965 MHz, 6538 GB/s and 1670 bf16 TFLOP/s measured).  Large products: the way from L2, which gives 9.9 TB/s to
+// 4096 rows over 8 groups, 8192 -> 4096 (tensor pipe 73 %), and under load the power limit: 8192^3 in 8 bits 336 us (3.3 POP/s; 360 in a long
+// run), in bf16 724 us (1.52 PFLOP/s, the library's product 677; 766 and 733 in a long run).  Few rows: the weight's bytes: 8 groups of 4 rows, 4096 ->
+// 14336, 146 us (6.4 TB/s); 16 rows, 8192 -> 28672 in 8 bits, 42 us (5.6 TB/s); below some 60 MB the 4 to 5 us that a launch,
+// the first copy's way and the last stores take: 4096 -> 14336 14 us, 4096 -> 4096 8 us.  Weight gradients of short groups: their stores, which
+// leave an SM at 32 bytes a cycle (32 groups of 31 rows, 2048 x 4096, bf16 106 us, 5.2 TB/s).
 //
 // Every operand is brought by tiled copies with the 128-byte swizzle, K-major where the contracted dimension is contiguous and
 // MN-major where it is not (w in GRAD_ROWS, both operands in GRAD_WEIGHTS: no transposed copy of anything is made).  Copies
@@ -544,7 +545,7 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             } else if (whole) {
                 const bool pairs = sizeof(Out) == 2 && P.pairs;
                 // (unrolled only where registers are indexed: four copies of the body missed the instruction cache: bf16 weight gradients of 32 groups
-                // of 31 rows, 2048 x 4096, 145 us, 118 this way)
+                // of 31 rows, 2048 x 4096, 145 us, 118 without)
 #pragma unroll (RUNS ? CHUNKS : 1)
                 for (int i = 0; i < CHUNKS; ++i) {
                     const int c0 = (2 * i + part) * 32;
