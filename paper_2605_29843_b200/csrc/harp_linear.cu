@@ -243,6 +243,7 @@ harp_status_t harp_processed_linear_i8(const harp_plan_t *plan_in, const harp_pl
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     void *own = nullptr;
     if (!scratch) {
+        const OutsideCapture outside;
         const size_t bytes = (size_t)harp_processed_linear_scratch_bytes(plan_in, n_rows);
         cudaMemPool_t pool = harp_scratch_pool(id);
         if ((pool ? cudaMallocFromPoolAsync(&own, bytes, pool, s) : cudaMallocAsync(&own, bytes, s)) != cudaSuccess) {

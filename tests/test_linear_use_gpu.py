@@ -220,6 +220,29 @@ assert torch.equal(y, z) and z.abs().sum() > 0
     subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), check=True, timeout=100)
 
 
+def test_a_captured_layer():
+    """The whole layer without scratch of the caller's, its first call captured, replayed on other rows."""
+    code = """
+import torch
+import paper_2605_29843_b200 as harp
+from paper_2605_29843_b200 import workloads as wl
+plan_in, plan_out = (harp.plan_from_spec(wl.tiny_plan(s, r, kind='qr', perm='identity', signs=True)) for s, r in ((3, (8, 8, 4)), (4, (8, 4, 4))))
+wq = torch.randint(-127, 128, (plan_out.d, plan_in.d), dtype=torch.int8, device='cuda')
+sw = torch.rand(plan_out.d, device='cuda')
+rows, y = torch.randn(2, 9, plan_in.d, device='cuda').bfloat16(), torch.empty(9, plan_out.d, dtype=torch.bfloat16, device='cuda')
+x = rows[0].clone()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    harp.processed_linear_i8(x, plan_in, plan_out, wq, sw, out=y)
+for r in rows:
+    x.copy_(r)
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(y, harp.processed_linear_i8(r.clone(), plan_in, plan_out, wq, sw)) and y.abs().sum() > 0
+"""
+    subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), check=True, timeout=100)
+
+
 @pytest.mark.parametrize("misaligned", [False, True])
 def test_two_graphs_and_two_streams_at_once(misaligned):
     sets = [_calls(1 + 10 * i, misaligned) for i in range(4)]
