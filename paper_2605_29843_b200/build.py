@@ -2,6 +2,7 @@
 _harpcall.abi3.so (the call from Python; ctypes does without it), in-tree, next to this file.  ``python -m paper_2605_29843_b200.build`` or build()."""
 from __future__ import annotations
 
+import fcntl
 import glob
 import os
 import subprocess
@@ -33,12 +34,34 @@ def _stale() -> bool:
     return any(os.path.getmtime(p) > t for p in deps)
 
 
+def _call_stale() -> bool:
+    return (not os.path.exists(CALL) or os.path.getmtime(CALL_SRC) > os.path.getmtime(CALL)) and \
+        os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h"))
+
+
+def _produce(cmd, target) -> None:
+    """What a command that was interrupted leaves is never taken for its result."""
+    part = target + ".part"
+    subprocess.check_call(cmd + ["-o", part])
+    os.replace(part, target)
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    headers = sysconfig.get_paths()["include"]
-    if (force or not os.path.exists(CALL) or os.path.getmtime(CALL_SRC) > os.path.getmtime(CALL)) and os.path.exists(os.path.join(headers, "Python.h")):
-        subprocess.check_call([os.environ.get("CC", "gcc"), "-shared", "-fPIC", "-O2", "-I", headers, CALL_SRC, "-o", CALL])
-    if not force and not _stale():
+    if not force and not _stale() and not _call_stale():
         return LIB
+    os.makedirs(OBJECTS, exist_ok=True)
+    with open(os.path.join(OBJECTS, "lock"), "w") as lock:        # one build of a tree at a time
+        fcntl.flock(lock, fcntl.LOCK_EX)
+        if force or _call_stale():
+            headers = sysconfig.get_paths()["include"]
+            if os.path.exists(os.path.join(headers, "Python.h")):
+                _produce([os.environ.get("CC", "gcc"), "-shared", "-fPIC", "-O2", "-I", headers, CALL_SRC], CALL)
+        if force or _stale():
+            _build_lib(force, verbose)
+    return LIB
+
+
+def _build_lib(force: bool, verbose: bool) -> None:
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     cmd = [nvcc, "-c", "-Xcompiler", "-fPIC", "-std=c++17", "-O3", "-lineinfo",
            "-gencode", "arch=compute_100a,code=sm_100a",
@@ -49,24 +72,29 @@ def build(force: bool = False, verbose: bool = False) -> str:
         cmd += ["-DHARP_TM_TIMING"]
     if os.environ.get("HARP_FAST_TIMING"):        # ... and in the whole-row kernel
         cmd += ["-DHARP_FAST_TIMING"]
-    # an object a source: several at a time, and those alone whose source or headers changed
-    os.makedirs(OBJECTS, exist_ok=True)
+    # An object a source: several at a time, and those alone whose source or headers changed.  Kept objects belong to the command and the
+    # compiler that the key names; it is gone while some may be of another one.
     headers_at = max(os.path.getmtime(p) for p in headers_of_sources())
-    flags = os.path.join(OBJECTS, "command")
-    same = os.path.exists(flags) and open(flags).read() == repr(cmd)
+    key_at, key = os.path.join(OBJECTS, "command"), repr(cmd) + subprocess.check_output([nvcc, "--version"], text=True)
+    if os.path.exists(key_at):
+        with open(key_at) as f:
+            force |= f.read() != key
+    else:
+        force = True
+    if force and os.path.exists(key_at):
+        os.remove(key_at)
 
     def compile_one(src):
         obj = os.path.join(OBJECTS, os.path.basename(src) + ".o")
-        if force or not same or not os.path.exists(obj) or os.path.getmtime(obj) < max(headers_at, os.path.getmtime(src)):
-            subprocess.check_call(cmd + [src, "-o", obj])
+        if force or not os.path.exists(obj) or os.path.getmtime(obj) < max(headers_at, os.path.getmtime(src)):
+            _produce(cmd + [src], obj)
         return obj
 
     with ThreadPoolExecutor(os.cpu_count() or 1) as pool:
         objects = list(pool.map(compile_one, sources()))
-    with open(flags, "w") as f:
-        f.write(repr(cmd))
-    subprocess.check_call([nvcc, "-shared", "-gencode", "arch=compute_100a,code=sm_100a", *objects, "-o", LIB])
-    return LIB
+    with open(key_at, "w") as f:
+        f.write(key)
+    _produce([nvcc, "-shared", "-gencode", "arch=compute_100a,code=sm_100a", *objects], LIB)
 
 
 if __name__ == "__main__":
