@@ -360,7 +360,10 @@ harp_status_t harp_grouped_linear_i8(const int8_t *x, int64_t ld_x, const float 
                                      int64_t d_in, int64_t d_out, void *y, int64_t ld_y, harp_dtype_t y_dtype, void *stream);
 
 /* y_r = x_r W_e^T for the rows of group e: x  DEVICE n_rows x d_in, w  DEVICE n_groups x d_out x d_in, both bf16;
- * y  DEVICE n_rows x d_out of y_dtype.  Products are summed in fp32 and rounded once, in an order that the sizes fix. */
+ * y  DEVICE n_rows x d_out of y_dtype.  Products are summed in fp32, in an order that the sizes fix, and the sum is rounded once to y_dtype.
+ * Sums within a run of products are cut off, not rounded (6e-9 of a sum of one sign a product at most, as measured); runs are added up rounding to
+ * nearest.  A run is of 512 products for an fp32 result and for bf16 results of more than 32768 products, else all of them.  This holds for
+ * the gradients below, too. */
 harp_status_t harp_grouped_linear(const void *x, int64_t ld_x, const void *w, int64_t ld_w, const int32_t *offsets,
                                   int32_t n_groups, int64_t n_rows, int64_t d_in, int64_t d_out, void *y, int64_t ld_y,
                                   harp_dtype_t y_dtype, void *stream);

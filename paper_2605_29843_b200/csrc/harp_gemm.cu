@@ -46,10 +46,14 @@ using namespace harp_gemm_ptx;
 
 constexpr int kThreads = 384;                // warps: 0 copies, 1 products, 2 tensor memory, 3 offsets, then both ragged ends, 4-11 epilogue (two a lane quarter)
 constexpr int kHalf = 16384;                 // the lane operand's part of a stage in one CTA
-// The tensor core cuts its fp32 sums off instead of rounding them, sixteen products at a time: the result of a long sum is too small by
-// 1.1e-9 of itself a product (1.6e-5 after 14336).  Results in fp32 are therefore summed in runs of 512 products, which the epilogue adds up,
-// rounding to nearest: 5e-7 at any length.  bf16 results round off 2^-9 in any case and take one run.
+// The tensor core cuts its fp32 sums off instead of rounding them: the sum of n products of one sign comes out too small by 1.4e-9 n of itself
+// after 512 of them, 4 to 6e-9 n from some thousand on (mixed signs: by chance, 1e-6 at most of the sum of magnitudes).  Results in fp32 are therefore summed in
+// runs of 512 products, which the epilogue adds up, rounding to nearest: 7 to 9e-7 too small, and 2^-24 at most for each run that is added.  bf16
+// results round off 2^-8 at most in any case and take one run of up to 32768 products (2e-4, a twentieth of that), whose sum the stores read where it lies.
+// Beyond that they take runs of 512 too (one run of 2^20: 6e-3), in kernels of their own: the registers that hold sums cost short sums too much (both gradients of 32
+// groups of 31 rows, 2048 x 4096, 218 -> 315 us in a kernel that could do either).
 constexpr int kRun = 8;                      // blocks
+constexpr int kLone = 32768;                 // products
 constexpr int kTurnBytes = 8 * 2048;         // where the epilogue warps of a pair's CTA turn bf16 results round
 constexpr int kSumCols = 32;                 // columns whose sums a split adds up at a time
 // COLS: most columns of a tile (256 for a pair of CTAs, 32 or 64 for one).  DEEP: a single CTA has the SM for itself, and the shared memory;
@@ -71,13 +75,15 @@ struct Params {
     int64_t ld_out, group_out;               // group_out: elements between two groups' outputs (GRAD_WEIGHTS)
     const float *row_scale, *channel_scale;
     int32_t accumulate;
+    int32_t above, most;                     // GRAD_WEIGHTS: groups of more rows than `above`, of `most` at most; the others are another launch's
     int32_t chunked_a, chunked_b;            // MN-major operands: both chunks of 64 by one copy
     int32_t pairs, eights;                   // bf16 results may be stored two, eight lanes at a time
     int32_t *err;
 };
 
 struct Tile {
-    int e, lane0, col0, cols, row0, blocks, tail;    // cols: valid ones; row0: first row; tail: rows in the last block (GRAD_WEIGHTS)
+    int e, lane0, col0, cols, row0, blocks, tail;    // cols: valid ones; row0: first row; tail: rows in the last block (GRAD_WEIGHTS);
+                                                     // blocks: -1 where the tile is another launch's
 };
 
 __device__ __forceinline__ int div_up(int a, int b) { return (a + b - 1) / b; }
@@ -139,6 +145,7 @@ struct Walk {
             T.row0 = off[e];
             T.blocks = div_up(rows, BLOCK);
             T.tail = rows - (T.blocks - 1) * BLOCK;
+            if (rows <= P.above || rows > P.most) T.blocks = -1;
         } else {
             T.cols = min(tile_cols, rows - T.col0);
             T.row0 = off[e] + T.col0;
@@ -197,7 +204,8 @@ __device__ __forceinline__ uint32_t pack_bf16(uint32_t lo, uint32_t hi) {
     return r;
 }
 
-template <bool I8, int COLS, bool DEEP, int PRODUCT, typename Out>
+// RUNS: sums of runs of blocks are added up in registers
+template <bool I8, int COLS, bool DEEP, int PRODUCT, typename Out, bool RUNS>
 __global__ void __launch_bounds__(kThreads, COLS == 256 || DEEP ? 1 : 2)
 harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                  const __grid_constant__ CUtensorMap map_b_small, const Params P) {
@@ -205,7 +213,6 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     constexpr int CG = COLS == 256 ? 2 : 1;                  // CTAs a tile
     constexpr int STAGES = stages(COLS, DEEP), kStage = stage_bytes(COLS);
     constexpr bool A_MN = PRODUCT != FORWARD, B_MN = PRODUCT == GRAD_WEIGHTS;
-    constexpr bool RUNS = !I8 && sizeof(Out) == 4;           // sums of runs of blocks are added up in registers
     constexpr int RUN = RUNS ? kRun : 1 << 30;
     constexpr uint32_t COLUMNS = 2 * COLS, ACC = COLS;       // two accumulators
 
@@ -398,7 +405,7 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         uint32_t phases = 0;                                 // a bit a stage: its next ragged block's phase
         for (int t = cluster; t < n_tiles; t += clusters) {
             const Tile T = tiles.at(t);
-            if (T.blocks == 0) continue;
+            if (T.blocks <= 0) continue;
             ring.skip(T.blocks - 1);
             if (is_ragged(T, T.blocks - 1)) {
                 if ((ring.s ^ warp) & 1) {
@@ -440,6 +447,7 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             Out *const out = static_cast<Out *>(P.out) +
                 (PRODUCT == GRAD_WEIGHTS ? T.e * P.group_out + (int64_t)T.col0 * P.ld_out : (int64_t)T.row0 * P.ld_out) + l;
             const float by_lane = I8 && inside ? P.channel_scale[(int64_t)T.e * P.lanes + l] : 1.0f;
+            if (PRODUCT == GRAD_WEIGHTS && T.blocks < 0) continue;
             if (T.blocks == 0) {                             // a group without rows
                 if (inside && !P.accumulate)
                     for (int c = part; c < T.cols; c += 2) store(out + (int64_t)c * P.ld_out, 0.0f);
@@ -489,7 +497,7 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 if (!alive) break;
             } else if (any && !arrived()) break;
             const uint32_t d = accumulator();
-            if (CG == 2 && sizeof(Out) == 2 && P.eights) {
+            if (CG == 2 && sizeof(Out) == 2 && !RUNS && P.eights) {
                 // Results as mma.sync's fragments, pairs of columns packed, turned round in shared memory: eight lanes of a column are 16 bytes there.
                 // A third of the instructions that storing lane by lane takes (8 bits, 16384 x 4096 x 14336 655 -> 619 us).
                 unsigned char *const turn = base_ptr + STAGES * kStage + (warp - 4) * 2048;      // 32 columns of 64 bytes
@@ -708,9 +716,9 @@ int smem_bytes(int cols, bool deep, int split, int n_groups) {
     return 1024 + stages(cols, deep) * stage_bytes(cols) + (cols == 256 ? kTurnBytes : split > 1 ? kSumCols * 512 : 0) + 8 * (n_groups + 1);
 }
 
-template <bool I8, int COLS, bool DEEP, int PRODUCT, typename Out>
+template <bool I8, int COLS, bool DEEP, int PRODUCT, typename Out, bool RUNS>
 harp_status_t launch(const CUtensorMap (&maps)[3], const Params &P, int clusters, cudaStream_t s) {
-    const auto kernel = harp_gemm_kernel<I8, COLS, DEEP, PRODUCT, Out>;
+    const auto kernel = harp_gemm_kernel<I8, COLS, DEEP, PRODUCT, Out, RUNS>;
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem) != cudaSuccess) return HARP_ERR_CUDA;
     const int size = COLS == 256 ? 2 : P.split;
     cudaLaunchConfig_t cfg = {};
@@ -736,8 +744,11 @@ harp_status_t launch(const CUtensorMap (&maps)[3], const Params &P, int clusters
 }
 
 template <bool I8, int COLS, bool DEEP, int PRODUCT>
-harp_status_t launch(harp_dtype_t out, const CUtensorMap (&maps)[3], const Params &P, int clusters, cudaStream_t s) {
-    return out == HARP_F32 ? launch<I8, COLS, DEEP, PRODUCT, float>(maps, P, clusters, s) : launch<I8, COLS, DEEP, PRODUCT, __nv_bfloat16>(maps, P, clusters, s);
+harp_status_t launch(harp_dtype_t out, bool runs, const CUtensorMap (&maps)[3], const Params &P, int clusters, cudaStream_t s) {
+    if (out == HARP_F32) return launch<I8, COLS, DEEP, PRODUCT, float, !I8>(maps, P, clusters, s);
+    if constexpr (!I8)
+        if (runs) return launch<I8, COLS, DEEP, PRODUCT, __nv_bfloat16, true>(maps, P, clusters, s);
+    return launch<I8, COLS, DEEP, PRODUCT, __nv_bfloat16, false>(maps, P, clusters, s);
 }
 
 // How a call is cut: by pairs of CTAs on 256 lanes x 256 columns, or by single ones on 128 x 32 or 128 x 64 in clusters of `split`.
@@ -810,9 +821,9 @@ bool describe(int dev, Device &d) {
                         cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess;
         return ok ? n : 0;
     };
-    d.pairs = resident(harp_gemm_kernel<false, 256, false, FORWARD, __nv_bfloat16>, 256, 2);
+    d.pairs = resident(harp_gemm_kernel<false, 256, false, FORWARD, __nv_bfloat16, false>, 256, 2);
     // (the query counts one CTA an SM wherever tensor memory is used; two of these fit, and run)
-    for (int i = 0; i < 3; ++i) d.clusters[i] = 2 * resident(harp_gemm_kernel<false, 32, false, FORWARD, __nv_bfloat16>, 32, 1 << i);
+    for (int i = 0; i < 3; ++i) d.clusters[i] = 2 * resident(harp_gemm_kernel<false, 32, false, FORWARD, __nv_bfloat16, false>, 32, 1 << i);
     d.err = static_cast<int32_t *>(err);
     return d.pairs > 0 && d.clusters[0] > 0 && d.clusters[1] > 0 && d.clusters[2] > 0;
 }
@@ -904,12 +915,24 @@ harp_status_t gemm(const Call &c, const Device &dev, cudaStream_t stream) {
     auto by_cols = [&](auto i8, auto product) {
         constexpr bool I8 = decltype(i8)::value;
         constexpr int PRODUCT = decltype(product)::value;
-        if (shape.cols == 256) return launch<I8, 256, false, PRODUCT>(c.out_dtype, maps, P, clusters, stream);
+        const bool runs = P.depth > kLone;
+        if (shape.cols == 256) return launch<I8, 256, false, PRODUCT>(c.out_dtype, runs, maps, P, clusters, stream);
         if (shape.cols == 64)
-            return deep ? launch<I8, 64, true, PRODUCT>(c.out_dtype, maps, P, clusters, stream) : launch<I8, 64, false, PRODUCT>(c.out_dtype, maps, P, clusters, stream);
-        return deep ? launch<I8, 32, true, PRODUCT>(c.out_dtype, maps, P, clusters, stream) : launch<I8, 32, false, PRODUCT>(c.out_dtype, maps, P, clusters, stream);
+            return deep ? launch<I8, 64, true, PRODUCT>(c.out_dtype, runs, maps, P, clusters, stream) : launch<I8, 64, false, PRODUCT>(c.out_dtype, runs, maps, P, clusters, stream);
+        return deep ? launch<I8, 32, true, PRODUCT>(c.out_dtype, runs, maps, P, clusters, stream) : launch<I8, 32, false, PRODUCT>(c.out_dtype, runs, maps, P, clusters, stream);
     };
-    if (c.product == GRAD_WEIGHTS) return launch<false, 256, false, GRAD_WEIGHTS>(c.out_dtype, maps, P, clusters, stream);
+    if (c.product == GRAD_WEIGHTS) {
+        // only the GPU knows how long the groups are: where one may be too long for a single run, a launch for either kind
+        P.above = -1;
+        P.most = INT32_MAX;
+        const bool two = c.out_dtype == HARP_BF16 && P.n_rows > kLone;
+        if (two) P.most = kLone;
+        const harp_status_t st = launch<false, 256, false, GRAD_WEIGHTS>(c.out_dtype, false, maps, P, clusters, stream);
+        if (!two || st != HARP_OK) return st;
+        P.above = kLone;
+        P.most = INT32_MAX;
+        return launch<false, 256, false, GRAD_WEIGHTS>(c.out_dtype, true, maps, P, clusters, stream);
+    }
     if (c.product == GRAD_ROWS) return by_cols(std::false_type(), std::integral_constant<int, GRAD_ROWS>());
     return c.i8 ? by_cols(std::true_type(), std::integral_constant<int, FORWARD>()) : by_cols(std::false_type(), std::integral_constant<int, FORWARD>());
 }
