@@ -318,7 +318,6 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     if (warp == 0 && lane == 0) {
         Tiles tiles(P, off, first);
         Ring<STAGES> ring;
-        uint32_t used = 0;                                   // a bit for each stage that a copy went to
         bool alive = true;
         for (int t = cluster; alive && t < n_tiles; t += clusters) {
             const Tile T = tiles.at(t);
@@ -338,7 +337,6 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 else if (CG == 1) mbar_expect_tx(bar, bytes);
                 else if (rank == 0) mbar_expect_tx(bar, 2 * bytes);
                 else bar = map_rank(bar, 0);
-                used |= 1u << s;
                 const int k = b * BLOCK;
                 if (PRODUCT == FORWARD) load_3d<CG>(a, &map_a, k, lane0, T.e, bar);
                 else if (PRODUCT == GRAD_ROWS && P.chunked_a) load_4d<CG>(a, &map_a, 0, k, lane0 / 64, T.e, bar);
@@ -357,11 +355,6 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
                 else
                     for (int i = 0; i < boxes; ++i) load_2d<CG>(bb + i * 4096, &map_b_small, k, T.row0 + col0 + i * 32, bar);
             }
-        }
-        if (!alive && (CG == 1 || rank == 0)) {
-            // leave no copy in flight, of either CTA: the last use of every stage, as far as there was one
-            for (int s = 0; s < STAGES; ++s)
-                for (uint32_t i = 0; (used >> s & 1) && i < kSpin && !mbar_try(full(s), s < ring.s ? ring.phase : ring.phase ^ 1); ++i) {}
         }
     } else if (warp == 1 && lane == 0 && (CG == 1 || rank == 0)) {
         Tiles tiles(P, off, first);
@@ -685,9 +678,21 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         }
     }
     __syncwarp();
+    // (the thread whose wait gave up reads what it has written itself)
+    for (int r = 0; *wait.dead && r < size; ++r) store_at(map_rank(smem_u32(&s_dead), r), 1);
+    __syncwarp();
     tc_fence_before();
     if (size > 1) cluster_sync();                            // the others' barriers and memory stay until all are done
     else __syncthreads();
+    if (*wait.dead) {
+        // A wait gave up, as all CTAs of the cluster know by now.  Copies, products and sums that were on their way count at barriers of either CTA that
+        // nobody need have armed, so no barrier tells when they have landed; they take microseconds.  All stay 10 ms longer with the memory that they go to.
+        const long long start = clock64();
+        for (int i = 0; threadIdx.x == 0 && i < 1 << 16 && clock64() - start < 20000000; ++i) __nanosleep(1000);
+        __syncwarp();
+        if (size > 1) cluster_sync();
+        else __syncthreads();
+    }
     if (warp == 2) {
         tc_fence_after();
         free_columns<CG, COLUMNS>(columns);
