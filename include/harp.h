@@ -390,6 +390,13 @@ harp_status_t harp_processed_linear_i8(const harp_plan_t *plan_in, const harp_pl
                                        void *scratch, void *stream);
 int64_t harp_processed_linear_scratch_bytes(const harp_plan_t *plan_in, int64_t n_rows);
 
+/* How the products are cut, for tests and measurements of each kernel (harp_apply_ex does this for the applies).  A tile is of `cols` columns:
+ * 256 by a pair of CTAs, or 32 or 64 by one, with clusters of `split` CTAs (1, 2, 4) that divide the contracted dimension and, if deep is 1 (64
+ * columns, or split 1), the longer of two rings of stages.  An estimate chooses unless the calling thread has set a cut for its calls; cols 0 takes
+ * it back.  Weight gradients always go by pairs.  HARP_ERR_BAD_DIM for any other cut.  harp_linear_last_cut: what the thread's last product took. */
+harp_status_t harp_linear_set_cut(int32_t cols, int32_t split, int32_t deep);
+void harp_linear_last_cut(int32_t cut[3]);
+
 /* Wait status of the product kernels on the current device, as harp_plan_error_word is for a plan's: 0 if no wait has given
  * up since the library was loaded.  Synchronises with the device. */
 int32_t harp_linear_error_word(void);

@@ -103,6 +103,10 @@ def lib() -> ctypes.CDLL:
         L.harp_processed_linear_i8.argtypes = [vp, vp, vp, i64, ci, vp, i64, vp, vp, vp, vp]
         L.harp_processed_linear_scratch_bytes.restype = i64
         L.harp_processed_linear_scratch_bytes.argtypes = [vp, i64]
+        L.harp_linear_set_cut.restype = ci
+        L.harp_linear_set_cut.argtypes = [i32, i32, i32]
+        L.harp_linear_last_cut.restype = None
+        L.harp_linear_last_cut.argtypes = [ctypes.POINTER(i32)]
         L.harp_linear_error_word.restype = i32
         L.harp_linear_error_word.argtypes = []
         L.harp_launch_count.restype = i64
@@ -432,6 +436,20 @@ def harp_processed_linear_i8(plan_in: Plan, plan_out: Plan, x_ptr: int, n_rows: 
 
 def harp_processed_linear_scratch_bytes(plan_in: Plan, n_rows: int) -> int:
     return int(lib().harp_processed_linear_scratch_bytes(plan_in.handle, int(n_rows)))
+
+
+def harp_linear_set_cut(cols: int, split: int = 1, deep: bool = False) -> None:
+    """The cut that this thread's products take from now on; cols 0: by estimate again."""
+    st = lib().harp_linear_set_cut(cols, split, 1 if deep else 0)
+    if st != HARP_OK:
+        raise HarpError(st, "harp_linear_set_cut")
+
+
+def harp_linear_last_cut():
+    """(cols, split, deep) of this thread's last product."""
+    cut = (ctypes.c_int32 * 3)()
+    lib().harp_linear_last_cut(cut)
+    return cut[0], cut[1], bool(cut[2])
 
 
 def harp_linear_error_word() -> int:

@@ -760,7 +760,18 @@ harp_status_t launch(harp_dtype_t out, bool runs, const CUtensorMap (&maps)[3], 
 struct Shape {
     int cols, split, slots;              // slots: clusters (pairs) that run at once
     int64_t tiles;                       // at most
+    bool deep;                           // the longer ring
 };
+struct Cut {
+    int32_t cols = 0, split = 1, deep = 0;
+};
+thread_local Cut asked, taken;           // by harp_linear_set_cut; by the last call
+
+int64_t lanes_of(const Call &c) { return c.product == FORWARD ? c.d_out : c.d_in; }
+int64_t most_tiles(const Call &c, int cols) {
+    const int64_t across = cols == 256 ? (lanes_of(c) + 255) / 256 : (lanes_of(c) + 127) / 128;
+    return across * ((c.n_rows + cols - 1) / cols + c.n_groups - 1);
+}
 
 // The cut with the least estimated time: the weight's bytes at the rate of memory, stretched by a last round of tiles that leaves SMs
 // idle, or rounds of tiles times their blocks of 128 contracted bytes.  Constants from 8-bit products of 1 to 2048 rows, widths 2048 to 28672,
@@ -775,9 +786,13 @@ struct Shape {
 //   8 x 16 rows, 4096 -> 14336   173.9   159.2  147.7  148.4      162.8  154.4  152.6     (bf16)
 //   64 x 64 rows, 2048 -> 2048    55.1    61.7   72.6  116.7       54.7   62.6  100.8
 Shape choose(const Call &c, const Device &dev) {
-    const int64_t lanes = c.product == FORWARD ? c.d_out : c.d_in, pair_tiles = (lanes + 255) / 256, tiles = (lanes + 127) / 128;
-    if (c.product == GRAD_WEIGHTS) return {256, 1, dev.pairs, c.n_groups * pair_tiles * ((c.d_out + 255) / 256)};
-    const Shape pairs = {256, 1, dev.pairs, pair_tiles * ((c.n_rows + 255) / 256 + c.n_groups - 1)};
+    const int64_t pair_tiles = (lanes_of(c) + 255) / 256, tiles = (lanes_of(c) + 127) / 128;
+    if (c.product == GRAD_WEIGHTS) return {256, 1, dev.pairs, c.n_groups * pair_tiles * ((c.d_out + 255) / 256), false};
+    if (asked.cols) {
+        const int slots = asked.cols == 256 ? dev.pairs : dev.clusters[asked.split / 2];
+        return {asked.cols, asked.split, slots, most_tiles(c, asked.cols), asked.deep != 0};
+    }
+    const Shape pairs = {256, 1, dev.pairs, most_tiles(c, 256), false};
     // rows of a group, and a quarter more where there are several: they are not even, but many fit a tile that the mean fits
     const int64_t met = std::min<int64_t>(c.n_groups, c.n_rows), even = (c.n_rows + met - 1) / met, rows = met > 1 ? even + even / 4 : even;
     const double blocks = (double)(((c.product == FORWARD ? c.d_in : c.d_out) * (c.i8 ? 1 : 2) + 127) / 128), memory = (double)(met * tiles) * blocks * 16384 / 6.3e6;     // us
@@ -799,9 +814,12 @@ Shape choose(const Call &c, const Device &dev) {
             const double t = std::max(memory * stretch + join, rounds * (blocks / (1 << i) * block + join)) + 3.5;
             if (t < least) {
                 least = t;
-                best = {cols, 1 << i, dev.clusters[i], tiles * ((c.n_rows + cols - 1) / cols + c.n_groups - 1)};
+                best = {cols, 1 << i, dev.clusters[i], most_tiles(c, cols), false};
             }
         }
+    // All tiles at once and one CTA an SM at most: a longer ring (1 row, 4096 -> 14336 14.9 -> 14.0 us, 64 rows 17.7 -> 15.3 us; clusters on
+    // 32 columns are better off with the next kernel's CTAs beside them, 1 row 4096 -> 4096 8.0 against 8.5 us).
+    best.deep = best.cols < 256 && best.tiles * best.split <= dev.sms && best.tiles <= best.slots / 2 && (best.split == 1 || best.cols == 64);
     return best;
 }
 
@@ -877,6 +895,7 @@ harp_status_t gemm(const Call &c, const Device &dev, cudaStream_t stream) {
     P.pairs = reinterpret_cast<uintptr_t>(c.out) % 4 == 0 && c.ld_out % 2 == 0 && P.lanes % 2 == 0 && !c.accumulate;
     P.eights = P.pairs && reinterpret_cast<uintptr_t>(c.out) % 16 == 0 && c.ld_out % 8 == 0 && P.lanes % 8 == 0;
     const Shape shape = choose(c, dev);
+    taken = {shape.cols, shape.split, shape.deep};
     if (shape.tiles > INT32_MAX / 16) return HARP_ERR_TOO_LARGE;
     P.tile_cols = shape.cols;
     P.split = shape.split;
@@ -914,17 +933,14 @@ harp_status_t gemm(const Call &c, const Device &dev, cudaStream_t stream) {
         ok = ok && encode(&maps[1], c.i8, c.rows, 2, e, p, box) && encode(&maps[2], c.i8, c.rows, 2, e, p, box_small);
     }
     if (!ok) return HARP_ERR_UNSUPPORTED;
-    // All tiles at once and one CTA an SM at most: a longer ring (1 row, 4096 -> 14336 14.9 -> 14.0 us, 64 rows 17.7 -> 15.3 us; clusters on
-    // 32 columns are better off with the next kernel's CTAs beside them, 1 row 4096 -> 4096 8.0 against 8.5 us).
-    const bool deep = shape.tiles * shape.split <= dev.sms && shape.tiles <= shape.slots / 2 && (shape.split == 1 || shape.cols == 64);
     auto by_cols = [&](auto i8, auto product) {
         constexpr bool I8 = decltype(i8)::value;
         constexpr int PRODUCT = decltype(product)::value;
         const bool runs = P.depth > kLone;
         if (shape.cols == 256) return launch<I8, 256, false, PRODUCT>(c.out_dtype, runs, maps, P, clusters, stream);
         if (shape.cols == 64)
-            return deep ? launch<I8, 64, true, PRODUCT>(c.out_dtype, runs, maps, P, clusters, stream) : launch<I8, 64, false, PRODUCT>(c.out_dtype, runs, maps, P, clusters, stream);
-        return deep ? launch<I8, 32, true, PRODUCT>(c.out_dtype, runs, maps, P, clusters, stream) : launch<I8, 32, false, PRODUCT>(c.out_dtype, runs, maps, P, clusters, stream);
+            return shape.deep ? launch<I8, 64, true, PRODUCT>(c.out_dtype, runs, maps, P, clusters, stream) : launch<I8, 64, false, PRODUCT>(c.out_dtype, runs, maps, P, clusters, stream);
+        return shape.deep ? launch<I8, 32, true, PRODUCT>(c.out_dtype, runs, maps, P, clusters, stream) : launch<I8, 32, false, PRODUCT>(c.out_dtype, runs, maps, P, clusters, stream);
     };
     if (c.product == GRAD_WEIGHTS) {
         // only the GPU knows how long the groups are: where one may be too long for a single run, a launch for either kind
@@ -943,3 +959,17 @@ harp_status_t gemm(const Call &c, const Device &dev, cudaStream_t stream) {
 }
 
 }  // namespace harp_linear
+
+extern "C" harp_status_t harp_linear_set_cut(int32_t cols, int32_t split, int32_t deep) {
+    const bool pairs = cols == 256 && split == 1 && deep == 0;
+    const bool single = (cols == 32 || cols == 64) && (split == 1 || split == 2 || split == 4) &&
+                        (deep == 0 || (deep == 1 && (split == 1 || cols == 64)));
+    if (cols != 0 && !pairs && !single) return HARP_ERR_BAD_DIM;
+    harp_linear::asked = {cols, split, deep};
+    return HARP_OK;
+}
+extern "C" void harp_linear_last_cut(int32_t cut[3]) {
+    cut[0] = harp_linear::taken.cols;
+    cut[1] = harp_linear::taken.split;
+    cut[2] = harp_linear::taken.deep;
+}
