@@ -724,7 +724,10 @@ int smem_bytes(int cols, bool deep, int split, int n_groups) {
 template <bool I8, int COLS, bool DEEP, int PRODUCT, typename Out, bool RUNS>
 harp_status_t launch(const CUtensorMap (&maps)[3], const Params &P, int clusters, cudaStream_t s) {
     const auto kernel = harp_gemm_kernel<I8, COLS, DEEP, PRODUCT, Out, RUNS>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem) != cudaSuccess) return HARP_ERR_CUDA;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem) != cudaSuccess) {
+        cudaGetLastError();
+        return HARP_ERR_CUDA;
+    }
     const int size = COLS == 256 ? 2 : P.split;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(clusters * size));

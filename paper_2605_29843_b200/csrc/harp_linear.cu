@@ -62,6 +62,12 @@ struct OutsideCapture {
     ~OutsideCapture() { cudaThreadExchangeStreamCaptureMode(&mode); }
 };
 
+// for a CUDA call that failed: nothing of it stays behind for the next one, and an earlier failure is the one to tell
+harp_status_t refused(harp_status_t earlier = HARP_OK) {
+    cudaGetLastError();
+    return earlier == HARP_OK ? HARP_ERR_CUDA : earlier;
+}
+
 harp_status_t run(Call c, cudaStream_t s) {
     const OutsideCapture outside;
     const Device *dev = device();
@@ -75,7 +81,7 @@ harp_status_t run(Call c, cudaStream_t s) {
         if (o.bad(es)) bytes += o.rows * o.pieces(es) * 16;
     if (bytes == 0) return gemm(c, *dev, s);
     int id = 0;
-    if (cudaGetDevice(&id) != cudaSuccess) return HARP_ERR_CUDA;
+    if (cudaGetDevice(&id) != cudaSuccess) return refused();
     cudaMemPool_t pool = harp_scratch_pool(id);
     void *scratch = nullptr;
     if ((pool ? cudaMallocFromPoolAsync(&scratch, (size_t)bytes, pool, s) : cudaMallocAsync(&scratch, (size_t)bytes, s)) != cudaSuccess) {
@@ -83,23 +89,34 @@ harp_status_t run(Call c, cudaStream_t s) {
         return HARP_ERR_ALLOC;
     }
     uint8_t *to = static_cast<uint8_t *>(scratch);
+    harp_status_t st = HARP_OK;
     for (const Operand &o : ops) {
         if (!o.bad(es)) continue;
         const bool weight = o.ptr == &c.other && c.product != GRAD_WEIGHTS;
         // 64 pieces of four rows a CTA, and as many CTAs as are resident at once
         const int64_t pieces = o.pieces(es), across = (pieces + 63) / 64;
         const int64_t down = std::max<int64_t>(1, std::min<int64_t>((o.rows + 3) / 4, (int64_t)dev->sms * 8 / across));
-        pad_rows_kernel<<<dim3((unsigned)across, (unsigned)down), dim3(64, 4), 0, s>>>(static_cast<const uint8_t *>(*o.ptr), *o.ld * es, o.rows, o.d * es, reinterpret_cast<uint4 *>(to), pieces,
-                                                           weight ? c.offsets : nullptr, c.d_out);
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)across, (unsigned)down);
+        cfg.blockDim = dim3(64, 4);
+        cfg.stream = s;
+        // (its own status: cudaGetLastError would tell what an earlier call of this thread left)
+        const cudaError_t err = cudaLaunchKernelEx(&cfg, pad_rows_kernel, static_cast<const uint8_t *>(*o.ptr), *o.ld * es, o.rows, o.d * es,
+                                                   reinterpret_cast<uint4 *>(to), pieces, weight ? c.offsets : nullptr, c.d_out);
         g_harp_launches.fetch_add(1, std::memory_order_relaxed);
+        if (err != cudaSuccess) {
+            st = refused();
+            break;
+        }
         *o.ptr = to;
         *o.ld = pieces * 16 / es;
         to += o.rows * pieces * 16;
     }
-    harp_status_t st = cudaGetLastError() == cudaSuccess ? gemm(c, *dev, s) : HARP_ERR_CUDA;
-    if (cudaFreeAsync(scratch, s) != cudaSuccess && st == HARP_OK) st = HARP_ERR_CUDA;
+    if (st == HARP_OK) st = gemm(c, *dev, s);
+    if (cudaFreeAsync(scratch, s) != cudaSuccess) st = refused(st);
     return st;
 }
+
 
 harp_status_t check_sizes(int64_t n_rows, int64_t d_in, int64_t d_out, int64_t n_groups) {
     if (n_rows < 0 || d_in < 1 || d_out < 1 || n_groups < 1) return HARP_ERR_BAD_DIM;
@@ -206,7 +223,7 @@ harp_status_t harp_grouped_grad_weights(const void *gy, int64_t ld_gy, const voi
     if (n_rows == 0) {
         const size_t es = harp_dtype_size(gw_dtype);
         if (accumulate) return HARP_OK;
-        return cudaMemset2DAsync(gw, (size_t)ld_gw * es, 0, (size_t)d_in * es, (size_t)n_groups * (size_t)d_out, s) == cudaSuccess ? HARP_OK : HARP_ERR_CUDA;
+        return cudaMemset2DAsync(gw, (size_t)ld_gw * es, 0, (size_t)d_in * es, (size_t)n_groups * (size_t)d_out, s) == cudaSuccess ? HARP_OK : refused();
     }
     Call c;
     c.product = GRAD_WEIGHTS;
@@ -238,7 +255,7 @@ harp_status_t harp_processed_linear_i8(const harp_plan_t *plan_in, const harp_pl
     if ((st = check_out(x, dtype)) != HARP_OK || (st = check_out(y, dtype)) != HARP_OK) return st;
     if (!aligned(w_scale, 4) || !aligned(scratch, 16)) return HARP_ERR_BAD_DIM;
     int id = -1;
-    if (cudaGetDevice(&id) != cudaSuccess) return HARP_ERR_CUDA;
+    if (cudaGetDevice(&id) != cudaSuccess) return refused();
     if (id != plan_in->device || id != plan_out->device) return HARP_ERR_DIM_MISMATCH;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     void *own = nullptr;
@@ -258,7 +275,7 @@ harp_status_t harp_processed_linear_i8(const harp_plan_t *plan_in, const harp_pl
     if (st == HARP_OK) st = harp_quantize_rows(x, d_in, n_rows, d_in, dtype, q, ld_q, scale, stream);
     if (st == HARP_OK) st = harp_linear_i8(q, ld_q, scale, w, ld_w, w_scale, n_rows, d_in, d_out, y, d_out, dtype, stream);
     if (st == HARP_OK) st = harp_apply(plan_out, y, n_rows, dtype, 1, stream);
-    if (own && cudaFreeAsync(own, s) != cudaSuccess && st == HARP_OK) st = HARP_ERR_CUDA;
+    if (own && cudaFreeAsync(own, s) != cudaSuccess) st = refused(st);
     return st;
 }
 
