@@ -330,8 +330,8 @@ int32_t harp_plan_error_word(const harp_plan_t *plan);
  * groups follow one another at n rows x ld.  Buffers are aligned to their element size.  Rows (bases and leading dimensions)
  * on 16-byte boundaries are read in place; others are copied first to scratch that the call takes on the
  * stream from the library's pool, so weights are best kept with a padded leading dimension.  Outputs must not overlap inputs.
- * d_in and d_out from 1 to 2^20 (8 bits: d_in to 131071, so that every sum fits 32 bits), up to 2^30 rows and 1024 groups:
- * beyond that HARP_ERR_TOO_LARGE.  No plan is involved: pointers belong to the current device.  n_rows == 0
+ * d_in and d_out from 1 to 2^20 (8 bits: d_in to 131071, so that every sum fits 32 bits), up to 2^30 rows and 1024 groups, leading dimensions
+ * to 2^37: beyond that HARP_ERR_TOO_LARGE (harp_quantize_rows: d to 2^20 and up to 2^31 - 1 rows, beyond that HARP_ERR_BAD_DIM).  No plan is involved: pointers belong to the current device.  n_rows == 0
  * returns HARP_OK without a launch, unless an output has to be cleared.  All are asynchronous on stream and may run on several
  * streams at once.
  *

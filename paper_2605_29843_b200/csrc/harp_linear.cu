@@ -9,7 +9,6 @@ namespace {
 using namespace harp_linear;
 
 constexpr int64_t kMostRows = 1ll << 30, kMostDim = 1ll << 20;
-constexpr int64_t kMostLd = 1ll << 37;           // the copy engine's rows lie less than 2^40 bytes apart
 constexpr int64_t kMostDepthI8 = 131071;         // 128 * 128 * d_in stays below 2^31
 
 bool aligned(const void *p, uintptr_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }

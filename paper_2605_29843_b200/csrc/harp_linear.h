@@ -12,6 +12,7 @@ namespace harp_linear {
 // Which of the three products of a layer: y = x W^T, dx = dy W, dW = dy^T x (per group).
 enum Product { FORWARD = 0, GRAD_ROWS = 1, GRAD_WEIGHTS = 2 };
 
+constexpr int64_t kMostLd = 1ll << 37;   // leading dimensions: the copy engine's rows lie less than 2^40 bytes apart
 constexpr int kMaxGroups = 1024;         // offsets and tile counts of all groups stay in shared memory
 
 // One call, after its checks.  `lanes` is the dimension that lies along the lanes of tensor memory and contiguous in the

@@ -236,6 +236,7 @@ extern "C" harp_status_t harp_quantize_rows(const void *x, int64_t ld_x, int64_t
                                             int8_t *q, int64_t ld_q, float *scale, void *stream) {
     if (dtype != HARP_F32 && dtype != HARP_BF16) return HARP_ERR_BAD_DTYPE;
     if (n_rows < 0 || n_rows > INT32_MAX || d < 1 || d > (1ll << 20) || ld_x < d || ld_q < d) return HARP_ERR_BAD_DIM;
+    if (ld_x > harp_linear::kMostLd || ld_q > harp_linear::kMostLd) return HARP_ERR_TOO_LARGE;
     if (n_rows == 0) return HARP_OK;
     if (!x || !q || !scale) return HARP_ERR_NULL;
     const uintptr_t es = dtype == HARP_F32 ? 4 : 2;
