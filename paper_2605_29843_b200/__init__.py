@@ -548,7 +548,8 @@ def _matrix(name, t, shape, dtypes, dim, device):
     if t.is_contiguous():
         return shape[-1]
     stride = t.stride()
-    ld = stride[-2] if shape[-2] > 1 else max(shape[-1], stride[-2])
+    # (a dimension of one has any stride: the leading dimension of weights of one row is the step between groups)
+    ld = stride[-2] if shape[-2] > 1 else stride[0] if dim == 3 and shape[0] > 1 else max(shape[-1], stride[-2])
     if (shape[-1] > 1 and stride[-1] != 1) or ld < shape[-1] or (dim == 3 and shape[0] > 1 and stride[0] != ld * shape[1]):
         raise ValueError(f"{name}: rows have to be contiguous and evenly spaced, got strides {stride}")
     return ld
