@@ -690,6 +690,8 @@ def grouped_grad_weights(gy, x, offsets, out=None, out_dtype=None, accumulate=Fa
     (n, d_out), (n_x, d_in), groups = gy_shape, x_shape, offsets.numel() - 1
     if n != n_x:
         raise ValueError(f"gy has {n} rows and x {n_x}")
+    if groups < 0:
+        raise ValueError("offsets: one value more than groups expected, got none")
     if accumulate and out is None:
         raise ValueError("accumulate needs out")
     _vector("offsets", offsets, _i32, groups + 1, device)

@@ -29,6 +29,14 @@ def test_weights_of_one_row(rows):
         harp.grouped_linear(x, base.as_strided((3, 1, d_in), (d_in - 1, d_in, 1)), off)
 
 
+def test_no_offsets():
+    x, gy, off = normal(1, 4, 8).to(torch.bfloat16), normal(2, 4, 8).to(torch.bfloat16), torch.empty(0, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        harp.grouped_grad_weights(gy, x, off)
+    with pytest.raises(harp.HarpError):
+        harp.grouped_grad_weights(gy, x, offsets_of([]))
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("d_out", [1, 2])
 def test_no_rows_and_results_far_apart(d_out, dtype):
