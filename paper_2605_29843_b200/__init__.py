@@ -620,7 +620,8 @@ def linear_i8(x, x_scale, w, w_scale, out=None, out_dtype=None):
 
 
 def grouped_linear_i8(x, x_scale, w, w_scale, offsets, out=None, out_dtype=None):
-    """linear_i8 with a weight per group of rows: w [groups, d_out, d_in], w_scale [groups, d_out], offsets int32 [groups + 1]."""
+    """linear_i8 with a weight per group of rows: w [groups, d_out, d_in], w_scale [groups, d_out], offsets int32 [groups + 1] on the GPU.  Rows
+    outside every group are not written: in a fresh result they hold anything."""
     if _apply_ex is None:
         _bind_torch()
     device = _current_device()
@@ -642,7 +643,7 @@ def grouped_linear_i8(x, x_scale, w, w_scale, offsets, out=None, out_dtype=None)
 
 def grouped_linear(x, w, offsets, out=None, out_dtype=None):
     """y_r = x_r w_e^T for offsets[e] <= r < offsets[e + 1]: bf16 x [n, d_in], w [groups, d_out, d_in], offsets int32 [groups + 1] on the
-    GPU; y is bf16 unless `out` or `out_dtype` says fp32.  Rows outside every group are not written."""
+    GPU; y is bf16 unless `out` or `out_dtype` says fp32.  Rows outside every group are not written: in a fresh result they hold anything."""
     if _apply_ex is None:
         _bind_torch()
     device = _current_device()
@@ -661,7 +662,8 @@ def grouped_linear(x, w, offsets, out=None, out_dtype=None):
 
 
 def grouped_grad_rows(gy, w, offsets, out=None, out_dtype=None):
-    """Gradient of grouped_linear with respect to its rows: gx_r = gy_r w_e."""
+    """Gradient of grouped_linear with respect to its rows: gx_r = gy_r w_e, bf16 unless `out` or `out_dtype` says fp32.  Rows outside every group
+    are not written: in a fresh result they hold anything."""
     if _apply_ex is None:
         _bind_torch()
     device = _current_device()
