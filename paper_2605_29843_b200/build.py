@@ -41,7 +41,7 @@ def _call_stale() -> bool:
 
 def _produce(cmd, target) -> None:
     """What a command that was interrupted leaves is never taken for its result."""
-    part = target + ".part"
+    part = os.path.join(OBJECTS, os.path.basename(target) + ".part")
     subprocess.check_call(cmd + ["-o", part])
     os.replace(part, target)
 

@@ -30,6 +30,8 @@ if [ $compile = 1 ]; then
   sleep ${DELAY:-0}
   echo "$src:$timing:$(cat "$(dirname "$0")/version")" > "$out"
 else
+  printf 'half of' > "$out"
+  [ "$FAIL_ON" = link ] && exit 1
   cat "${objects[@]}" > "$out"
 fi
 """
@@ -98,6 +100,16 @@ def test_a_compile_that_failed_leaves_no_object(tree, monkeypatch):
     with pytest.raises(subprocess.CalledProcessError):
         harp_build.build()
     assert not (tree / "_build" / "b.cu.o").exists() and not (tree / "lib.so").exists()
+    monkeypatch.delenv("FAIL_ON")
+    harp_build.build()
+    assert sorted(p.name for p in tree.iterdir()) == ["_build", "call.so", "compiled", "csrc", "lib.so", "nvcc", "version"]
+
+
+def test_a_link_that_failed_leaves_nothing_beside_the_sources(tree, monkeypatch):
+    monkeypatch.setenv("FAIL_ON", "link")
+    with pytest.raises(subprocess.CalledProcessError):
+        harp_build.build()
+    assert not [p.name for p in tree.iterdir() if p.name.startswith("lib")]
 
 
 def test_another_compiler_at_the_same_path(tree):
