@@ -51,7 +51,7 @@ constexpr int kHalf = 16384;                 // the lane operand's part of a sta
 // runs of 512 products, which the epilogue adds up, rounding to nearest: 7 to 9e-7 too small, and 2^-24 at most for each run that is added.  bf16
 // results round off 2^-8 at most in any case and take one run of up to 32768 products (2e-4, a twentieth of that), whose sum the stores read where it lies.
 // Beyond that they take runs of 512 too (one run of 2^20: 6e-3), in kernels of their own: the registers that hold sums cost short sums too much (both gradients of 32
-// groups of 31 rows, 2048 x 4096, 218 -> 315 us in a kernel that could do either).
+// groups of 31 rows, 2048 x 4096, 218 -> 315 us in a kernel that could do either).  Weight gradients of 65536 rows, 2048 x 4096, 786 us as one run, 865 now.
 constexpr int kRun = 8;                      // blocks
 constexpr int kLone = 32768;                 // products
 constexpr int kTurnBytes = 8 * 2048;         // where the epilogue warps of a pair's CTA turn bf16 results round
@@ -492,7 +492,8 @@ harp_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             const uint32_t d = accumulator();
             if (CG == 2 && sizeof(Out) == 2 && !RUNS && P.eights) {
                 // Results as mma.sync's fragments, pairs of columns packed, turned round in shared memory: eight lanes of a column are 16 bytes there.
-                // A third of the instructions that storing lane by lane takes (8 bits, 16384 x 4096 x 14336 655 -> 619 us).
+                // A third of the instructions that storing lane by lane takes (8 bits, 16384 x 4096 x 14336 655 -> 619 us in
+                // short bursts; 690 in a long run, at the power limit).
                 unsigned char *const turn = base_ptr + STAGES * kStage + (warp - 4) * 2048;      // 32 columns of 64 bytes
                 const uint32_t turn_s = smem_u32(turn);
                 auto place = [](int c, int eight) { return c * 64 + ((eight ^ (c >> 1 & 3)) << 4); };
